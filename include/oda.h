@@ -346,6 +346,73 @@ oda_status_t oda_full_decode_gated(oda_ctx_t* ctx, int32_t layer_begin, int32_t 
                                    float* lse, void* stream);
 
 /*
+ * The gated Full pass for a batch whose requests share long prefixes (one system prompt, one document asked many
+ * questions; the paper times one request at a time and has no counterpart).  Same result as
+ * oda_full_decode_gated, but the positions that all requests of a group share are read once for the group, as one
+ * matrix product over the rows of all its requests, instead of once per request.
+ *   group_start [num_groups + 1] i32, group_prefix [num_groups] i32 (device): requests group_start[i] ..
+ *     group_start[i+1]-1 hold the same tokens at positions 0 .. group_prefix[i]-1, and the same K and V there: whole
+ *     pages of the prefix are read through the block table of the group's first flagged request (usually all rows of
+ *     the table name the same pages; copies are fine).  A page that the prefix ends in, and everything behind it, is
+ *     read through each request's own row, so every row must be complete.  Requests in no group share nothing.
+ *     group_start must not fall and must stay within [0, batch]: a group that breaks this sets bit 3 of the device
+ *     status word and shares nothing (its results stay right).  A prefix longer than a flagged request is cut to
+ *     what leaves that request one position of its own; negative ones count as 0.
+ *   flags, out, lse: as in oda_full_decode_gated.  0 <= num_groups <= 128, empty groups
+ *     allowed; with 0 both arrays may be NULL.
+ *   scratch: device, 256-byte aligned, oda_full_decode_shared_scratch_bytes(ctx) bytes, used only during the call.
+ * Groups, lengths and flags are read on the device: one captured graph serves every prefix and every gate.  Always
+ * computes from scratch (options bit 1 has no effect).  TMA variant only.
+ */
+size_t oda_full_decode_shared_scratch_bytes(const oda_ctx_t* ctx);
+oda_status_t oda_full_decode_shared(oda_ctx_t* ctx, int32_t layer_begin, int32_t layer_end, int32_t batch,
+                                    const void* q_full, const void* k_cache, const void* v_cache,
+                                    const int32_t* block_table, const int32_t* seq_lens, const uint8_t* flags,
+                                    int32_t num_groups, const int32_t* group_start, const int32_t* group_prefix,
+                                    void* out, float* lse, void* scratch, size_t scratch_bytes, void* stream);
+
+/*
+ * The gated Full pass that also adds up how much every position was attended to:
+ *   weights[slice, b, g, j] += sum over the query heads h of KV head g of  e^{z_hj - lse_h},   0 <= j < t,
+ * for flagged requests on gated layers (slice = the layer's kv_index; layers that share a slice add to the same
+ * values, in layer order).  out and lse are those of oda_full_decode_gated.  The paper drops these weights; summed
+ * over the recalled steps they say which part of the history still matters (see oda_evict).
+ *   weights: [slices][max_batch][kv_heads][max_blocks_per_seq * 16] fp32 device, slices = 1 + the largest kv_index;
+ *     the caller zeroes a request's part when it starts.  Positions >= t and other requests are left as they were.
+ *   scratch: device, 256-byte aligned, at least oda_full_decode_weighted_scratch_bytes(ctx, 1, batch) bytes; with
+ *     room for n layers the call takes n layers at a time (two launches each time).
+ * No atomics: the same call gives the same bits.  Always computes from scratch (options bit 1 has no effect).
+ * TMA variant only.
+ */
+size_t oda_full_decode_weighted_scratch_bytes(const oda_ctx_t* ctx, int32_t layers, int32_t batch);
+oda_status_t oda_full_decode_weighted(oda_ctx_t* ctx, int32_t layer_begin, int32_t layer_end, int32_t batch,
+                                      const void* q_full, const void* k_cache, const void* v_cache,
+                                      const int32_t* block_table, const int32_t* seq_lens, const uint8_t* flags,
+                                      float* weights, void* out, float* lse, void* scratch, size_t scratch_bytes,
+                                      void* stream);
+
+/*
+ * Eviction: shortens every request with seq_lens[b] = t > budget (and mask[b] != 0; mask NULL = all) to `budget`
+ * positions.  For each cache slice and KV head by itself it keeps the first `sinks` positions, the last `recent`
+ * ones and, of those between them, the budget - sinks - recent with the largest weights (of equal ones the earliest;
+ * -0 = 0, NaN counts as larger than everything), and moves their K, V and weights to positions 0 .. budget-1 in
+ * their old order; weights budget .. t-1 become 0, and seq_lens[b] becomes budget.  Keys stay rotated as they were.
+ *   kept (nullable): [slices][batch][kv_heads][budget] i32, the old position of every new one; a request within the
+ *     budget gets 0 .. t-1 and then -1, a masked one is not written.  Without it the list needs scratch (device,
+ *     256-byte aligned, oda_evict_scratch_bytes(ctx) suffices for every budget); with it scratch may be NULL.
+ *   weights: as in oda_full_decode_weighted.  All slices of the cache are treated, those of fixed-window layers too:
+ *     choose `recent` at least as large as the largest window, and what a Local pass reads stays what it was.
+ * The rows move inside the request's own pages: no other request may use a page of a request that is shortened
+ * (a shared prefix is copied before its first eviction).  Pages behind the budget are free afterwards; the block table
+ * is not changed.  Requires 1 <= budget <= max_blocks_per_seq * 16 and 0 <= sinks + recent <= budget.  A request with
+ * t < 1 or beyond the table sets the device status word and is skipped.  Two launches; nothing synchronises.
+ */
+size_t oda_evict_scratch_bytes(const oda_ctx_t* ctx);
+oda_status_t oda_evict(oda_ctx_t* ctx, int32_t batch, float* weights, void* k_cache, void* v_cache,
+                       const int32_t* block_table, int32_t* seq_lens, const uint8_t* mask, int32_t budget,
+                       int32_t sinks, int32_t recent, int32_t* kept, void* scratch, size_t scratch_bytes, void* stream);
+
+/*
  * Commit of the current token (Algorithm 1, line 8; the fused KV commitment of the appendix on
  * selected-state execution): for every layer and every request with mask[b] != 0 (mask NULL =
  * all), writes k_cur/v_cur[l,b,:,:] ([L,B,Hkv,D] bf16) into the paged cache at position

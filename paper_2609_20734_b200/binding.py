@@ -28,6 +28,8 @@ EXPORTS = [
     "oda_write_current_kv", "oda_select_rows", "oda_advance_seq_lens", "oda_full_head_param_count", "oda_full_head_scratch_bytes",
     "oda_recall_score_full", "oda_recall_score_full_pre", "oda_recall_preact", "oda_recall_finalize", "oda_merge_partials",
     "oda_recall_finalize_exchange", "oda_merge_partials_exchange", "oda_set_cache_resident_bytes",
+    "oda_full_decode_shared", "oda_full_decode_shared_scratch_bytes", "oda_full_decode_weighted",
+    "oda_full_decode_weighted_scratch_bytes", "oda_evict", "oda_evict_scratch_bytes",
 ]
 
 
@@ -124,6 +126,16 @@ def load_library():
         lib.oda_set_cache_resident_bytes.argtypes = [vp, ctypes.c_size_t]
         lib.oda_set_cache_resident_bytes.restype = i32
         lib.oda_full_decode_gated.argtypes = [vp, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp]
+        sz = ctypes.c_size_t
+        lib.oda_full_decode_shared.argtypes = [vp, i32, i32, i32, vp, vp, vp, vp, vp, vp, i32, vp, vp, vp, vp, vp, sz, vp]
+        lib.oda_full_decode_weighted.argtypes = [vp, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        lib.oda_evict.argtypes = [vp, i32, vp, vp, vp, vp, vp, vp, i32, i32, i32, vp, vp, sz, vp]
+        lib.oda_full_decode_shared_scratch_bytes.argtypes = [vp]
+        lib.oda_full_decode_shared_scratch_bytes.restype = sz
+        lib.oda_full_decode_weighted_scratch_bytes.argtypes = [vp, i32, i32]
+        lib.oda_full_decode_weighted_scratch_bytes.restype = sz
+        lib.oda_evict_scratch_bytes.argtypes = [vp]
+        lib.oda_evict_scratch_bytes.restype = sz
         lib.oda_step.argtypes = [vp, ctypes.POINTER(_StepArgs), vp]
         lib.oda_step_host.argtypes = [vp, ctypes.POINTER(_StepArgs), vp,
                                       ctypes.POINTER(ctypes.c_size_t), ctypes.POINTER(ctypes.c_size_t)]
@@ -216,6 +228,10 @@ def _ptr(t) -> Optional[int]:
         return t.ctypes.data
     assert t.is_contiguous(), "tensors handed to the library must be contiguous"
     return t.data_ptr()
+
+
+def _is_i32(t) -> bool:
+    return t.element_size() == 4 and not t.is_floating_point()
 
 
 def _stream() -> int:
@@ -345,6 +361,82 @@ class OdaContext:
             self._h, layer_begin, layer_end, batch, _ptr(q_full), _ptr(k_cache), _ptr(v_cache),
             _ptr(block_table), _ptr(seq_lens), _ptr(flags), _ptr(out), _ptr(lse),
             _stream() if stream is None else stream), "oda_full_decode_gated")
+
+    # ---- shared prefix, accumulated weights, eviction ---------------------------------
+    def full_decode_shared(self, layer_begin, layer_end, batch, q_full, k_cache, v_cache, block_table, seq_lens, flags,
+                           group_start, group_prefix, out, lse=None, scratch=None, stream=None):
+        """full_decode_gated for requests that share prefixes: group i (requests group_start[i] ..
+        group_start[i+1]-1) holds the same first group_prefix[i] positions, read once for the group.
+        `scratch`: from full_decode_shared_scratch(), made here if None."""
+        n = 0 if group_prefix is None else group_prefix.numel()
+        if n and (group_start.numel() != n + 1 or not _is_i32(group_start) or not _is_i32(group_prefix)):
+            raise ValueError("group_start [n + 1] and group_prefix [n] are int32 tensors")
+        if scratch is None:
+            scratch = self.full_decode_shared_scratch()
+        self._check(self.lib.oda_full_decode_shared(
+            self._h, layer_begin, layer_end, batch, _ptr(q_full), _ptr(k_cache), _ptr(v_cache), _ptr(block_table),
+            _ptr(seq_lens), _ptr(flags), n, _ptr(group_start), _ptr(group_prefix), _ptr(out), _ptr(lse), _ptr(scratch),
+            scratch.numel(), _stream() if stream is None else stream), "oda_full_decode_shared")
+
+    def full_decode_shared_scratch(self, device="cuda"):
+        import torch
+
+        return torch.empty(self.lib.oda_full_decode_shared_scratch_bytes(self._h), dtype=torch.uint8, device=device)
+
+    def full_decode_weighted(self, layer_begin, layer_end, batch, q_full, k_cache, v_cache, block_table, seq_lens,
+                             flags, weights, out, lse=None, scratch=None, stream=None):
+        """full_decode_gated that also adds every position's attention weight to `weights`
+        [slices, max_batch, kv_heads, max_blocks_per_seq * 16] fp32.  `scratch`: from
+        full_decode_weighted_scratch(), made here if None."""
+        self._check_weights(weights)
+        if scratch is None:
+            scratch = self.full_decode_weighted_scratch()
+        self._check(self.lib.oda_full_decode_weighted(
+            self._h, layer_begin, layer_end, batch, _ptr(q_full), _ptr(k_cache), _ptr(v_cache), _ptr(block_table),
+            _ptr(seq_lens), _ptr(flags), _ptr(weights), _ptr(out), _ptr(lse), _ptr(scratch), scratch.numel(),
+            _stream() if stream is None else stream), "oda_full_decode_weighted")
+
+    def full_decode_weighted_scratch(self, layers=None, batch=None, most=1 << 30, device="cuda"):
+        """Scratch for the weighted pass: all layers at a time, or as many as `most` bytes hold (one at least)."""
+        import torch
+
+        batch = self.cfg.max_batch if batch is None else batch
+        one = self.lib.oda_full_decode_weighted_scratch_bytes(self._h, 1, batch)
+        if layers is None:
+            layers = max(1, min(self.cfg.num_layers, most // max(one, 1)))
+        return torch.empty(one * layers, dtype=torch.uint8, device=device)
+
+    def evict(self, batch, weights, k_cache, v_cache, block_table, seq_lens, budget, sinks=0, recent=0, mask=None,
+              kept=None, scratch=None, stream=None):
+        """Shortens every request of more than `budget` positions to its first `sinks`, its last `recent` and its
+        heaviest ones between them, per cache slice and KV head.  kept: [slices, batch, kv_heads, budget] int32,
+        the old positions of the new ones.  Without `kept` the list goes to `scratch` (evict_scratch())."""
+        self._check_weights(weights)
+        if kept is not None and (not _is_i32(kept) or kept.numel() != self.kv_slices * batch * self.cfg.num_kv_heads * budget):
+            raise ValueError("kept is an int32 tensor [slices, batch, kv_heads, budget]")
+        if kept is None and scratch is None:
+            scratch = self.evict_scratch()
+        self._check(self.lib.oda_evict(
+            self._h, batch, _ptr(weights), _ptr(k_cache), _ptr(v_cache), _ptr(block_table), _ptr(seq_lens), _ptr(mask),
+            int(budget), int(sinks), int(recent), _ptr(kept), _ptr(scratch), 0 if scratch is None else scratch.numel(),
+            _stream() if stream is None else stream), "oda_evict")
+
+    def evict_scratch(self, device="cuda"):
+        import torch
+
+        return torch.empty(self.lib.oda_evict_scratch_bytes(self._h), dtype=torch.uint8, device=device)
+
+    @property
+    def kv_slices(self) -> int:
+        """Cache slices the layers use (1 + the largest kv_index)."""
+        idx = self.cfg.layer_kv_index
+        return self.cfg.num_layers if idx is None else max(int(i) for i in idx) + 1
+
+    def _check_weights(self, w):
+        c = self.cfg
+        if w.element_size() != 4 or not w.is_floating_point() or \
+                w.numel() != self.kv_slices * c.max_batch * c.num_kv_heads * c.max_blocks_per_seq * c.block_size:
+            raise ValueError("weights is an fp32 tensor [slices, max_batch, kv_heads, max_blocks_per_seq * 16]")
 
     def recall_score_full(self, batch, params, d_tower, d_ff, n_blocks, h_prev, emb, h_local, threshold,
                           override_flags, scores, logits, flags, counters=None, eps=1e-6, scratch=None,

@@ -129,11 +129,17 @@ oda_status_t check_attn_args(oda_ctx* c, int lb, int le, int batch, const void* 
     return ODA_OK;
 }
 
+// what the passes that build on the gated Full pass add to its launch
+struct AttnExtra {
+    float* score_rows = nullptr;   // weighted pass: see AttnParams
+    float2* score_ml = nullptr;
+};
+
 oda_status_t launch_attention(oda_ctx* c, int mode, int lb, int le, int batch, const void* q,
                               const void* k, const void* v, const int32_t* bt, const int32_t* sl,
                               const uint8_t* flags, void* out, float* lse, cudaStream_t st,
                               int32_t* advance = nullptr, bool* advanced = nullptr,
-                              const oda_step_args_t* publish = nullptr)
+                              const oda_step_args_t* publish = nullptr, const AttnExtra* extra = nullptr)
 {
     const oda_config_t& f = c->cfg;
     AttnParams p;
@@ -210,6 +216,10 @@ oda_status_t launch_attention(oda_ctx* c, int mode, int lb, int le, int batch, c
         p.sm_claims = reinterpret_cast<int32_t*>(c->ws + c->lay.sm_claims);
     }
     if (advanced) *advanced = advance != nullptr;
+    if (extra) {
+        p.score_rows = extra->score_rows;
+        p.score_ml = extra->score_ml;
+    }
     // A Local call over few layers cannot fill the usual grid: the window bounds its pages whatever
     // the lengths are.  Launch only the CTAs the plan can give a span to (it cuts the page axis into
     // min(grid, max(1, pages / min_span_pages)) spans either way, so the split and the bits are the same);
@@ -1070,6 +1080,155 @@ oda_status_t oda_read_device_status(oda_ctx_t* c, void* stream, int32_t* code)
     if (e != cudaSuccess) return cuda_fail(c, e, "status read");
     *code = v;
     return v ? ODA_ERR_DEVICE_STATUS : ODA_OK;
+}
+
+// ---------------------------------------------------------------- shared prefix, accumulated weights, eviction
+
+static size_t weighted_layer_rows_bytes(const oda_ctx* c, int batch)
+{
+    return align_up((size_t)batch * c->cfg.num_q_heads * c->cfg.max_blocks_per_seq * kPage * sizeof(float));
+}
+static size_t weighted_layer_bytes(const oda_ctx* c, int batch)
+{
+    return weighted_layer_rows_bytes(c, batch) + align_up((size_t)batch * c->cfg.num_q_heads * sizeof(float2));
+}
+
+size_t oda_full_decode_weighted_scratch_bytes(const oda_ctx_t* c, int32_t layers, int32_t batch)
+{
+    if (!c || layers < 1 || batch < 1 || layers > c->cfg.num_layers || batch > c->cfg.max_batch) return 0;
+    return (size_t)layers * weighted_layer_bytes(c, batch);
+}
+
+oda_status_t oda_full_decode_weighted(oda_ctx_t* c, int32_t lb, int32_t le, int32_t batch, const void* q,
+                                      const void* k, const void* v, const int32_t* bt, const int32_t* sl,
+                                      const uint8_t* flags, float* weights, void* out, float* lse, void* scratch,
+                                      size_t scratch_bytes, void* stream)
+{
+    oda_status_t s = check_attn_args(c, lb, le, batch, q, k, v, bt, sl, out);
+    if (s != ODA_OK || batch == 0 || lb == le) return s;
+    if (!flags || !weights) return fail(c, ODA_ERR_INVALID_ARG, "flags or weights is null");
+    if (c->variant != ODA_VARIANT_TMA_MMA)
+        return fail(c, ODA_ERR_UNSUPPORTED, "the weighted Full pass exists in the TMA variant only");
+    if (!scratch || (reinterpret_cast<uintptr_t>(scratch) % kAlign) != 0)
+        return fail(c, ODA_ERR_WORKSPACE, "scratch is null or not 256-byte aligned");
+    const size_t rows = weighted_layer_rows_bytes(c, batch), per = weighted_layer_bytes(c, batch);
+    const int fit = (int)std::min<size_t>(scratch_bytes / per, (size_t)(le - lb));
+    if (fit < 1) return fail(c, ODA_ERR_WORKSPACE, "scratch holds not one layer (oda_full_decode_weighted_scratch_bytes)");
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    for (int l0 = lb; l0 < le; l0 += fit) {  // as many layers at a time as the scratch holds
+        const int l1 = std::min(l0 + fit, (int)le);
+        WeightParams w;
+        std::memset(&w, 0, sizeof w);
+        int n_slices = 0;
+        int last[kWeightMaxLayers];  // of each slice met so far: its latest layer
+        for (int l = l0; l < l1; ++l) {
+            w.next_layer[l - l0] = -1;
+            if (!c->layers[l].gated) continue;
+            int i = 0;
+            while (i < n_slices && w.slice[i] != c->layers[l].kv_index) ++i;
+            if (i == n_slices) {
+                w.slice[n_slices] = (uint16_t)c->layers[l].kv_index;
+                w.first_layer[n_slices++] = (int16_t)(l - l0);
+            } else {
+                w.next_layer[last[i]] = (int16_t)(l - l0);
+            }
+            last[i] = l - l0;
+        }
+        if (n_slices == 0) continue;
+        AttnExtra x;
+        x.score_rows = static_cast<float*>(scratch);
+        x.score_ml = reinterpret_cast<float2*>(static_cast<char*>(scratch) + (size_t)(l1 - l0) * rows);
+        s = launch_attention(c, 1, l0, l1, batch, q, k, v, bt, sl, flags, out, lse, st, nullptr, nullptr, nullptr, &x);
+        if (s != ODA_OK) return s;
+        w.score_rows = x.score_rows;
+        w.score_ml = x.score_ml;
+        w.weights = weights;
+        w.seq_lens = sl;
+        w.flags = flags;
+        w.batch = batch;
+        w.max_batch = c->cfg.max_batch;
+        w.num_kv_heads = c->cfg.num_kv_heads;
+        w.max_blocks_per_seq = c->cfg.max_blocks_per_seq;
+        cudaError_t e = launch_accumulate_weights(w, n_slices, c->group, st, c->use_pdl);
+        if (e != cudaSuccess) return cuda_fail(c, e, "weight accumulation launch");
+        c->launches += 1;
+    }
+    return ODA_OK;
+}
+
+size_t oda_evict_scratch_bytes(const oda_ctx_t* c)
+{
+    if (!c) return 0;
+    return (size_t)c->phys_layers * c->cfg.max_batch * c->cfg.num_kv_heads * c->cfg.max_blocks_per_seq * kPage * sizeof(int32_t);
+}
+
+oda_status_t oda_evict(oda_ctx_t* c, int32_t batch, float* weights, void* k, void* v, const int32_t* bt, int32_t* sl,
+                       const uint8_t* mask, int32_t budget, int32_t sinks, int32_t recent, int32_t* kept, void* scratch,
+                       size_t scratch_bytes, void* stream)
+{
+    if (!c) return ODA_ERR_INVALID_ARG;
+    const oda_config_t& f = c->cfg;
+    if (batch < 0 || batch > f.max_batch) return fail(c, ODA_ERR_INVALID_ARG, "batch outside [0, max_batch]");
+    if (budget < 1 || (long long)budget > (long long)f.max_blocks_per_seq * kPage)
+        return fail(c, ODA_ERR_INVALID_ARG, "budget outside [1, max_blocks_per_seq * 16]");
+    if (sinks < 0 || recent < 0 || (long long)sinks + recent > budget)
+        return fail(c, ODA_ERR_INVALID_ARG, "sinks and recent must fit the budget");
+    if (!c->ws) return fail(c, ODA_ERR_WORKSPACE, "oda_set_workspace has not been called");
+    if (batch == 0) return ODA_OK;
+    if (!weights || !k || !v || !bt || !sl) return fail(c, ODA_ERR_INVALID_ARG, "null pointer");
+    if (!aligned16(k) || !aligned16(v)) return fail(c, ODA_ERR_INVALID_ARG, "the caches must be 16-byte aligned");
+    if (!kept) {
+        const size_t need = (size_t)c->phys_layers * batch * f.num_kv_heads * budget * sizeof(int32_t);
+        if (!scratch || (reinterpret_cast<uintptr_t>(scratch) % kAlign) != 0 || scratch_bytes < need)
+            return fail(c, ODA_ERR_WORKSPACE, "without `kept` a 256-byte aligned scratch of oda_evict_scratch_bytes() is needed");
+        kept = static_cast<int32_t*>(scratch);
+    }
+    EvictParams p;
+    std::memset(&p, 0, sizeof p);
+    p.weights = weights;
+    p.k = static_cast<__nv_bfloat16*>(k);
+    p.v = static_cast<__nv_bfloat16*>(v);
+    p.block_table = bt;
+    p.seq_lens = sl;
+    p.mask = mask;
+    p.kept = kept;
+    p.status = reinterpret_cast<int32_t*>(c->ws + c->lay.status);
+    p.done = reinterpret_cast<int32_t*>(c->ws + c->lay.status + 32);
+    p.kv_layer_stride = f.kv_layer_stride;
+    p.kv_block_stride = f.kv_block_stride;
+    p.kv_token_stride = f.kv_token_stride;
+    p.kv_head_stride = f.kv_head_stride;
+    p.num_slices = c->phys_layers;
+    p.batch = batch;
+    p.max_batch = f.max_batch;
+    p.num_kv_heads = f.num_kv_heads;
+    p.max_blocks_per_seq = f.max_blocks_per_seq;
+    p.budget = budget;
+    p.sinks = sinks;
+    p.recent = recent;
+    cudaError_t e = launch_evict(p, f.head_dim, static_cast<cudaStream_t>(stream), c->use_pdl);
+    if (e != cudaSuccess) return cuda_fail(c, e, "eviction launch");
+    c->launches += 2;
+    return ODA_OK;
+}
+
+size_t oda_full_decode_shared_scratch_bytes(const oda_ctx_t* c) { return c ? kAlign : 0; }
+
+oda_status_t oda_full_decode_shared(oda_ctx_t* c, int32_t lb, int32_t le, int32_t batch, const void* q, const void* k,
+                                    const void* v, const int32_t* bt, const int32_t* sl, const uint8_t* flags,
+                                    int32_t num_groups, const int32_t* group_start, const int32_t* group_prefix,
+                                    void* out, float* lse, void* scratch, size_t scratch_bytes, void* stream)
+{
+    oda_status_t s = check_attn_args(c, lb, le, batch, q, k, v, bt, sl, out);
+    if (s != ODA_OK || batch == 0 || lb == le) return s;
+    if (!flags) return fail(c, ODA_ERR_INVALID_ARG, "flags is null");
+    if (num_groups < 0 || num_groups > kMaxBatch) return fail(c, ODA_ERR_INVALID_ARG, "num_groups outside [0, 128]");
+    if (num_groups > 0 && (!group_start || !group_prefix)) return fail(c, ODA_ERR_INVALID_ARG, "group_start or group_prefix is null");
+    if (!scratch || (reinterpret_cast<uintptr_t>(scratch) % kAlign) != 0 || scratch_bytes < oda_full_decode_shared_scratch_bytes(c))
+        return fail(c, ODA_ERR_WORKSPACE, "scratch is null, misaligned or smaller than oda_full_decode_shared_scratch_bytes()");
+    if (c->variant != ODA_VARIANT_TMA_MMA)
+        return fail(c, ODA_ERR_UNSUPPORTED, "the shared-prefix Full pass exists in the TMA variant only");
+    return launch_attention(c, 1, lb, le, batch, q, k, v, bt, sl, flags, out, lse, static_cast<cudaStream_t>(stream));
 }
 
 }  // extern "C"

@@ -67,6 +67,10 @@ struct AttnParams {
     int32_t* exit_counter;      // CTAs past their claim; zero between launches
     unsigned long long* sm_stats;  // calibration run: per SM (pages streamed, nanoseconds); else nullptr
     int32_t num_sms;
+    // Weighted Full pass (the score instance of the kernel): the logits of the pass, in log2 units, and
+    // what turns them into weights once a row is finished.  Layers count from layer_begin.
+    float* score_rows;          // [layers][batch][kv heads][max positions][group]
+    float2* score_ml;           // [layers][batch][q heads]: (m, 1 / l), weight = 2^(logit - m) / l
 };
 
 // Programmatic dependent launch: a kernel launched with the stream-serialisation attribute may

@@ -1,5 +1,6 @@
 // Host-side launch interface between the C-ABI layer (oda_api.cu) and the kernel files.
 #pragma once
+#include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
 
@@ -62,6 +63,39 @@ cudaError_t launch_merge_partials(const float* parts_out, const float* parts_lse
                                   const uint8_t* flags, const LayerInfo* layers, float* out, float* lse, int n_parts, int layer_begin,
                                   int layer_end, int batch, int q_heads, int head_dim, int num_layers,
                                   cudaStream_t st, bool pdl = false);
+
+// Weighted Full pass, second kernel: logits of the launch's gated layers -> accumulated weights (cache_weights.cu).
+constexpr int kWeightMaxLayers = 256;
+struct WeightParams {
+    const float* score_rows;     // [layers][batch][kv heads][max positions][group], log2 units
+    const float2* score_ml;      // [layers][batch][q heads]
+    float* weights;              // [slices][max_batch][kv heads][max positions]
+    const int32_t* seq_lens;
+    const uint8_t* flags;
+    int32_t batch, max_batch, num_kv_heads, max_blocks_per_seq;
+    // grid.z walks the cache slices that the launch's gated layers use: the slice, its first layer, and from
+    // each layer the next one on the same slice (-1: none).  Layers count from the launch's first.
+    int16_t first_layer[kWeightMaxLayers], next_layer[kWeightMaxLayers];
+    uint16_t slice[kWeightMaxLayers];
+};
+cudaError_t launch_accumulate_weights(const WeightParams& p, int n_slices, int group, cudaStream_t st, bool pdl = false);
+
+// Eviction down to a budget (cache_evict.cu): selection, then the move.
+struct EvictParams {
+    float* weights;              // [slices][max_batch][kv heads][max positions]
+    __nv_bfloat16* k;
+    __nv_bfloat16* v;
+    const int32_t* block_table;
+    int32_t* seq_lens;
+    const uint8_t* mask;         // nullable
+    int32_t* kept;               // [slices][batch][kv heads][budget]
+    int32_t* status;
+    int32_t* done;               // zero between launches
+    int64_t kv_layer_stride, kv_block_stride, kv_token_stride, kv_head_stride;
+    int32_t num_slices, batch, max_batch, num_kv_heads, max_blocks_per_seq;
+    int32_t budget, sinks, recent;
+};
+cudaError_t launch_evict(const EvictParams& p, int head_dim, cudaStream_t st, bool pdl = false);
 
 struct HeadParams {
     const float* feat_ext;      // [B, d_ext] or nullptr

@@ -149,15 +149,23 @@ struct PageRun {
     int take;
 };
 
-// kUniform = true: the instance launched for batch-1 Local calls over layers of one class that do not
-// qualify for one unit per CTA (a call over one or a few layers): it can take its equal split in closed
-// form from the one length.  The other instance does not carry that code.
-template <int D, int G, bool kUniform>
+// Instances of the kernel:
+//  kInstUniform  launched for batch-1 Local calls over layers of one class that do not qualify for one
+//                unit per CTA (a call over one or a few layers): it can take its equal split in closed
+//                form from the one length.  The others do not carry that code.
+//  kInstScores   the weighted Full pass: it also writes its logits (fp32, group x 4 bytes a position
+//                beside 4 D bytes of K and V) and each row's (m, 1 / l) for the kernel that adds the
+//                weights up.  It keeps P as three bf16 parts: 24 bits, so that fp32 results are as good
+//                as fp32 arithmetic makes them (two parts leave 1.6e-6 of the result; the third product
+//                is hidden behind the stream).
+constexpr int kInstGeneral = 0, kInstUniform = 1, kInstScores = 2;
+template <int D, int G, int kInst>
 __global__ void __launch_bounds__(TmaCfg<D>::kThreads, 2)
 splitkv_tma_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtensorMap kmap,
                    const __grid_constant__ CUtensorMap vmap, const int blocks_per_layer)
 {
     using C = TmaCfg<D>;
+    constexpr bool kUniform = kInst == kInstUniform;
     extern __shared__ __align__(1024) uint8_t smem[];
     uint8_t* ring = smem;                                                 // kStages * kStageBytes
     uint8_t* qring = ring + C::kStages * C::kStageBytes;                  // kStages * kQSlotBytes
@@ -386,6 +394,10 @@ splitkv_tma_kernel(const __grid_constant__ AttnParams p, const __grid_constant__
                     }
                 }
                 if (p.lse && hrow == 0) p.lse[lidx] = (mm + log2f(ll)) * kLn2;
+                if constexpr (kInst == kInstScores) {
+                    if (hrow == 0)
+                        p.score_ml[((size_t)(it.layer - p.layer_begin) * p.batch + it.b) * p.num_q_heads + h] = make_float2(mm, inv);
+                }
             }
         };
         for (uint32_t k = 0;; ++k) {
@@ -587,6 +599,20 @@ splitkv_tma_kernel(const __grid_constant__ AttnParams p, const __grid_constant__
                         mk0 = (v0 ? 0x0000ffffu : 0u) | (v1 ? 0xffff0000u : 0u);
                         mk1 = (v2 ? 0x0000ffffu : 0u) | (v3 ? 0xffff0000u : 0u);
                     }
+                    if constexpr (kInst == kInstScores) {
+                        // logits of the page: 16 tokens x G heads, one run of 64 G bytes (-inf outside the set)
+                        if (qc < G) {
+                            const size_t unit = ((size_t)(it.layer - p.layer_begin) * p.batch + it.b) * p.num_kv_heads + it.g;
+                            float* sc = p.score_rows + (unit * ((size_t)p.max_blocks_per_seq * kPage) + pos0 + hrow) * G + qc;
+                            if constexpr (G == 1) {
+                                sc[0] = x0s;
+                                sc[8] = x2s;
+                            } else {
+                                *reinterpret_cast<float2*>(sc) = make_float2(x0s, x1s);
+                                *reinterpret_cast<float2*>(sc + 8 * G) = make_float2(x2s, x3s);
+                            }
+                        }
+                    }
                     // ---- online softmax over the 16 tokens (fp32, base 2); tokens live across lanes ----
                     float mxA = fmaxf(x0s, x2s), mxB = fmaxf(x1s, x3s);
 #pragma unroll
@@ -612,6 +638,15 @@ splitkv_tma_kernel(const __grid_constant__ AttnParams p, const __grid_constant__
                     const uint32_t lo1 = pack_bf16x2(p2 - __uint_as_float(hi1 << 16), p3 - __uint_as_float(hi1 & 0xffff0000u));
                     const uint32_t bh0 = movmatrix_t(hi0), bh1 = movmatrix_t(hi1);
                     const uint32_t bl0 = movmatrix_t(lo0), bl1 = movmatrix_t(lo1);
+                    uint32_t bt0 = 0, bt1 = 0;  // third part of P
+                    if constexpr (kInst >= kInstScores) {
+                        const float r0 = p0 - __uint_as_float(hi0 << 16) - __uint_as_float(lo0 << 16);
+                        const float r1 = p1 - __uint_as_float(hi0 & 0xffff0000u) - __uint_as_float(lo0 & 0xffff0000u);
+                        const float r2 = p2 - __uint_as_float(hi1 << 16) - __uint_as_float(lo1 << 16);
+                        const float r3 = p3 - __uint_as_float(hi1 & 0xffff0000u) - __uint_as_float(lo1 & 0xffff0000u);
+                        bt0 = movmatrix_t(pack_bf16x2(r0, r1));
+                        bt1 = movmatrix_t(pack_bf16x2(r2, r3));
+                    }
                     // ---- O^T += V^T P^T ----
 #pragma unroll
                     for (int mt = 0; mt < D / 16; ++mt) {
@@ -624,6 +659,7 @@ splitkv_tma_kernel(const __grid_constant__ AttnParams p, const __grid_constant__
                         }
                         mma16816(o[mt], a0, a1, a2, a3, bh0, bh1);
                         mma16816(o[mt], a0, a1, a2, a3, bl0, bl1);
+                        if constexpr (kInst >= kInstScores) mma16816(o[mt], a0, a1, a2, a3, bt0, bt1);
                     }
                 }
                 __syncwarp();
@@ -797,45 +833,48 @@ bool encode_kv_map(void* out_map, const void* base, int head_dim, int num_kv_hea
     return r == CUDA_SUCCESS;
 }
 
+template <int D, int G, int kInst>
+static cudaError_t prepare_tma_t()
+{
+    cudaError_t e = cudaFuncSetAttribute(splitkv_tma_kernel<D, G, kInst>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                         TmaCfg<D>::kSmemBytes);
+    if (e != cudaSuccess) return e;
+    (void)cudaFuncSetAttribute(splitkv_tma_kernel<D, G, kInst>, cudaFuncAttributePreferredSharedMemoryCarveout,
+                               cudaSharedmemCarveoutMaxShared);
+    return cudaSuccess;
+}
+
 template <int D, int G>
 static cudaError_t launch_tma_t(const AttnParams& p, const void* kmap, const void* vmap, int blocks_per_layer,
                                 int grid, cudaStream_t st, bool pdl)
 {
     static bool attr_set = false;
     if (!attr_set) {
-        cudaError_t e = cudaFuncSetAttribute(splitkv_tma_kernel<D, G, false>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                             TmaCfg<D>::kSmemBytes);
-        if (e == cudaSuccess)
-            e = cudaFuncSetAttribute(splitkv_tma_kernel<D, G, true>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                     TmaCfg<D>::kSmemBytes);
+        cudaError_t e = prepare_tma_t<D, G, kInstGeneral>();
+        if (e == cudaSuccess) e = prepare_tma_t<D, G, kInstUniform>();
+        if (e == cudaSuccess) e = prepare_tma_t<D, G, kInstScores>();
         if (e != cudaSuccess) return e;
-        (void)cudaFuncSetAttribute(splitkv_tma_kernel<D, G, false>, cudaFuncAttributePreferredSharedMemoryCarveout,
-                                   cudaSharedmemCarveoutMaxShared);
-        (void)cudaFuncSetAttribute(splitkv_tma_kernel<D, G, true>, cudaFuncAttributePreferredSharedMemoryCarveout,
-                                   cudaSharedmemCarveoutMaxShared);
         attr_set = true;
     }
+    const CUtensorMap& km = *reinterpret_cast<const CUtensorMap*>(kmap);
+    const CUtensorMap& vm = *reinterpret_cast<const CUtensorMap*>(vmap);
+    const dim3 g(grid), t(TmaCfg<D>::kThreads);
+    if (p.score_rows)
+        return launch_ex(splitkv_tma_kernel<D, G, kInstScores>, g, t, TmaCfg<D>::kSmemBytes, st, pdl, p, km, vm, blocks_per_layer);
     if (p.uniform_hint && !p.direct_hint)
-        return launch_ex(splitkv_tma_kernel<D, G, true>, dim3(grid), dim3(TmaCfg<D>::kThreads), TmaCfg<D>::kSmemBytes, st,
-                         pdl, p, *reinterpret_cast<const CUtensorMap*>(kmap), *reinterpret_cast<const CUtensorMap*>(vmap),
-                         blocks_per_layer);
-    return launch_ex(splitkv_tma_kernel<D, G, false>, dim3(grid), dim3(TmaCfg<D>::kThreads), TmaCfg<D>::kSmemBytes, st, pdl,
-                     p, *reinterpret_cast<const CUtensorMap*>(kmap), *reinterpret_cast<const CUtensorMap*>(vmap),
-                     blocks_per_layer);
+        return launch_ex(splitkv_tma_kernel<D, G, kInstUniform>, g, t, TmaCfg<D>::kSmemBytes, st, pdl, p, km, vm, blocks_per_layer);
+    return launch_ex(splitkv_tma_kernel<D, G, kInstGeneral>, g, t, TmaCfg<D>::kSmemBytes, st, pdl, p, km, vm, blocks_per_layer);
 }
 
 template <int D, int G>
 static int occupancy_tma_t()
 {
     int n = 0;
-    if (cudaFuncSetAttribute(splitkv_tma_kernel<D, G, false>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                             TmaCfg<D>::kSmemBytes) != cudaSuccess) {
+    if (prepare_tma_t<D, G, kInstGeneral>() != cudaSuccess) {
         (void)cudaGetLastError();
         return 0;
     }
-    (void)cudaFuncSetAttribute(splitkv_tma_kernel<D, G, false>, cudaFuncAttributePreferredSharedMemoryCarveout,
-                               cudaSharedmemCarveoutMaxShared);
-    cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, splitkv_tma_kernel<D, G, false>, TmaCfg<D>::kThreads,
+    cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, splitkv_tma_kernel<D, G, kInstGeneral>, TmaCfg<D>::kThreads,
                                                   TmaCfg<D>::kSmemBytes);
     return n;
 }
