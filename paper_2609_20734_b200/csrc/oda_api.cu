@@ -13,6 +13,7 @@
 #include "../../include/oda.h"
 #include "oda_device.cuh"
 #include "oda_launch.h"
+#include "shared_prefix.cuh"
 
 using namespace oda;
 
@@ -53,6 +54,8 @@ struct oda_ctx {
     // TMA variant: tensor maps of the two caches, re-encoded when a base pointer changes
     alignas(64) unsigned char kmap[128];
     alignas(64) unsigned char vmap[128];
+    alignas(64) unsigned char kslab_map[128];  // K by 64-wide slabs (shared-prefix kernel)
+    const void* kslab_base = nullptr;
     const void* kmap_base = nullptr;
     const void* vmap_base = nullptr;
     int phys_layers = 1;
@@ -129,10 +132,23 @@ oda_status_t check_attn_args(oda_ctx* c, int lb, int le, int batch, const void* 
     return ODA_OK;
 }
 
+// tensor map of a cache, encoded again when the base pointer has changed
+bool refresh_map(oda_ctx* c, void* map, const void** base, const void* cache, int box_slabs)
+{
+    const oda_config_t& f = c->cfg;
+    if (*base == cache) return true;
+    if (!encode_kv_map(map, cache, f.head_dim, f.num_kv_heads, f.kv_token_stride, f.kv_head_stride, f.kv_block_stride,
+                       c->blocks_bound, box_slabs))
+        return false;
+    *base = cache;
+    return true;
+}
+
 // what the passes that build on the gated Full pass add to its launch
 struct AttnExtra {
     float* score_rows = nullptr;   // weighted pass: see AttnParams
     float2* score_ml = nullptr;
+    const SharedParams* shared = nullptr;  // tails of requests that share prefixes
 };
 
 oda_status_t launch_attention(oda_ctx* c, int mode, int lb, int le, int batch, const void* q,
@@ -219,6 +235,14 @@ oda_status_t launch_attention(oda_ctx* c, int mode, int lb, int le, int batch, c
     if (extra) {
         p.score_rows = extra->score_rows;
         p.score_ml = extra->score_ml;
+        if (const SharedParams* sp = extra->shared) {
+            p.page_shift = sp->page_shift;
+            p.seq_lens = sp->tail_lens;
+            p.shared = sp->desc;
+            p.shared_o = sp->part_o;
+            p.shared_ml = sp->part_ml;
+            p.shared_ext_row0 = sp->ext_row0;
+        }
     }
     // A Local call over few layers cannot fill the usual grid: the window bounds its pages whatever
     // the lengths are.  Launch only the CTAs the plan can give a span to (it cuts the page axis into
@@ -253,18 +277,8 @@ oda_status_t launch_attention(oda_ctx* c, int mode, int lb, int le, int batch, c
     }
     cudaError_t e;
     if (c->variant == ODA_VARIANT_TMA_MMA) {
-        if (c->kmap_base != k) {
-            if (!encode_kv_map(c->kmap, k, f.head_dim, f.num_kv_heads, f.kv_token_stride, f.kv_head_stride,
-                               f.kv_block_stride, c->blocks_bound))
-                return fail(c, ODA_ERR_CUDA, "cuTensorMapEncodeTiled failed for k_cache");
-            c->kmap_base = k;
-        }
-        if (c->vmap_base != v) {
-            if (!encode_kv_map(c->vmap, v, f.head_dim, f.num_kv_heads, f.kv_token_stride, f.kv_head_stride,
-                               f.kv_block_stride, c->blocks_bound))
-                return fail(c, ODA_ERR_CUDA, "cuTensorMapEncodeTiled failed for v_cache");
-            c->vmap_base = v;
-        }
+        if (!refresh_map(c, c->kmap, &c->kmap_base, k, 0)) return fail(c, ODA_ERR_CUDA, "cuTensorMapEncodeTiled failed for k_cache");
+        if (!refresh_map(c, c->vmap, &c->vmap_base, v, 0)) return fail(c, ODA_ERR_CUDA, "cuTensorMapEncodeTiled failed for v_cache");
         e = launch_splitkv_tma(p, c->kmap, c->vmap, c->blocks_per_layer, f.head_dim, c->group, grid, st, c->use_pdl);
     } else {
         e = launch_splitkv_simt(p, f.head_dim, c->group, grid, st, c->use_pdl);
@@ -1212,7 +1226,27 @@ oda_status_t oda_evict(oda_ctx_t* c, int32_t batch, float* weights, void* k, voi
     return ODA_OK;
 }
 
-size_t oda_full_decode_shared_scratch_bytes(const oda_ctx_t* c) { return c ? kAlign : 0; }
+struct SharedScratch {
+    size_t desc, shift, tails, ml, o, total, ext_row0;
+};
+static SharedScratch shared_scratch(const oda_ctx* c)
+{
+    const oda_config_t& f = c->cfg;
+    SharedScratch w;
+    size_t off = 0;
+    auto take = [&](size_t bytes) { size_t o = off; off = align_up(off + bytes); return o; };
+    w.desc = take(sizeof(SharedDesc));
+    w.shift = take(kMaxBatch * sizeof(int32_t));
+    w.tails = take(kMaxBatch * sizeof(int32_t));
+    w.ext_row0 = (size_t)f.num_layers * f.max_batch * f.num_q_heads;
+    const size_t rows = w.ext_row0 + (size_t)c->num_sms * 256;  // and the rows of one block for every span
+    w.ml = take(rows * sizeof(float2));
+    w.o = take(rows * f.head_dim * sizeof(float));
+    w.total = off;
+    return w;
+}
+
+size_t oda_full_decode_shared_scratch_bytes(const oda_ctx_t* c) { return c ? shared_scratch(c).total : 0; }
 
 oda_status_t oda_full_decode_shared(oda_ctx_t* c, int32_t lb, int32_t le, int32_t batch, const void* q, const void* k,
                                     const void* v, const int32_t* bt, const int32_t* sl, const uint8_t* flags,
@@ -1224,11 +1258,51 @@ oda_status_t oda_full_decode_shared(oda_ctx_t* c, int32_t lb, int32_t le, int32_
     if (!flags) return fail(c, ODA_ERR_INVALID_ARG, "flags is null");
     if (num_groups < 0 || num_groups > kMaxBatch) return fail(c, ODA_ERR_INVALID_ARG, "num_groups outside [0, 128]");
     if (num_groups > 0 && (!group_start || !group_prefix)) return fail(c, ODA_ERR_INVALID_ARG, "group_start or group_prefix is null");
-    if (!scratch || (reinterpret_cast<uintptr_t>(scratch) % kAlign) != 0 || scratch_bytes < oda_full_decode_shared_scratch_bytes(c))
-        return fail(c, ODA_ERR_WORKSPACE, "scratch is null, misaligned or smaller than oda_full_decode_shared_scratch_bytes()");
     if (c->variant != ODA_VARIANT_TMA_MMA)
         return fail(c, ODA_ERR_UNSUPPORTED, "the shared-prefix Full pass exists in the TMA variant only");
-    return launch_attention(c, 1, lb, le, batch, q, k, v, bt, sl, flags, out, lse, static_cast<cudaStream_t>(stream));
+    if (!scratch || (reinterpret_cast<uintptr_t>(scratch) % kAlign) != 0 || scratch_bytes < oda_full_decode_shared_scratch_bytes(c))
+        return fail(c, ODA_ERR_WORKSPACE, "scratch is null, misaligned or smaller than oda_full_decode_shared_scratch_bytes()");
+    const oda_config_t& f = c->cfg;
+    const SharedScratch w = shared_scratch(c);
+    char* base = static_cast<char*>(scratch);
+    SharedParams p;
+    std::memset(&p, 0, sizeof p);
+    for (int l = lb; l < le; ++l)
+        if (c->layers[l].gated) {
+            p.layer[p.num_gated] = (uint8_t)l;
+            p.kv_index[p.num_gated++] = (uint16_t)c->layers[l].kv_index;
+        }
+    if (p.num_gated == 0) return ODA_OK;
+    p.q = static_cast<const __nv_bfloat16*>(q);
+    p.block_table = bt;
+    p.seq_lens = sl;
+    p.flags = flags;
+    p.group_start = group_start;
+    p.group_prefix = group_prefix;
+    p.status = reinterpret_cast<int32_t*>(c->ws + c->lay.status);
+    p.desc = reinterpret_cast<SharedDesc*>(base + w.desc);
+    p.page_shift = reinterpret_cast<int32_t*>(base + w.shift);
+    p.tail_lens = reinterpret_cast<int32_t*>(base + w.tails);
+    p.part_ml = reinterpret_cast<float2*>(base + w.ml);
+    p.part_o = reinterpret_cast<float*>(base + w.o);
+    p.ext_row0 = w.ext_row0;
+    p.batch = batch;
+    p.num_groups = num_groups;
+    p.num_q_heads = f.num_q_heads;
+    p.num_kv_heads = f.num_kv_heads;
+    p.group = c->group;
+    p.max_blocks_per_seq = f.max_blocks_per_seq;
+    p.blocks_per_layer = c->blocks_per_layer;
+    p.scale_log2e = c->scale * 1.4426950408889634f;
+    if (!refresh_map(c, c->kslab_map, &c->kslab_base, k, 1)) return fail(c, ODA_ERR_CUDA, "cuTensorMapEncodeTiled failed for k_cache");
+    if (!refresh_map(c, c->vmap, &c->vmap_base, v, 0)) return fail(c, ODA_ERR_CUDA, "cuTensorMapEncodeTiled failed for v_cache");
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    cudaError_t e = launch_shared_prefix(p, c->kslab_map, c->vmap, f.head_dim, f.out_dtype != 0, c->num_sms, st, c->use_pdl);
+    if (e != cudaSuccess) return cuda_fail(c, e, "shared-prefix kernel launch");
+    c->launches += 1;
+    AttnExtra x;
+    x.shared = &p;
+    return launch_attention(c, 1, lb, le, batch, q, k, v, bt, sl, flags, out, lse, st, nullptr, nullptr, nullptr, &x);
 }
 
 }  // extern "C"

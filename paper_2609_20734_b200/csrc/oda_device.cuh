@@ -16,11 +16,14 @@ constexpr int kPartHdr = 4;        // a partial row is (m, l, -, -, o[D]): o sta
 
 // device status bits
 constexpr int kStatusBadSeqLen = 1;
-constexpr int kStatusItemOverflow = 2;
+constexpr int kStatusItemOverflow = 2;  // (4: kStatusWaitTimeout, mbar.cuh)
+constexpr int kStatusBadGroup = 8;      // shared-prefix groups out of order or outside the batch
 
 struct LayerInfo {  // one per layer, in the workspace
     int32_t window, sinks, gated, kv_index, cls, pad0, pad1, pad2;
 };
+
+struct SharedDesc;
 
 struct AttnParams {
     const __nv_bfloat16* q;
@@ -71,6 +74,13 @@ struct AttnParams {
     // what turns them into weights once a row is finished.  Layers count from layer_begin.
     float* score_rows;          // [layers][batch][kv heads][max positions][group]
     float2* score_ml;           // [layers][batch][q heads]: (m, 1 / l), weight = 2^(logit - m) / l
+    // Full pass over the tails of requests that share prefixes (the fold instance): pages of the table that a
+    // request skips, and where the partial results over its prefix are (shared_prefix.cuh)
+    const int32_t* page_shift;  // [batch]
+    const SharedDesc* shared;
+    const float* shared_o;
+    const float2* shared_ml;
+    size_t shared_ext_row0;
 };
 
 // Programmatic dependent launch: a kernel launched with the stream-serialisation attribute may

@@ -19,6 +19,7 @@
 #include "launch_ex.cuh"
 #include "mbar.cuh"
 #include "oda_launch.h"
+#include "shared_prefix.cuh"
 
 namespace oda {
 
@@ -158,7 +159,10 @@ struct PageRun {
 //                weights up.  It keeps P as three bf16 parts: 24 bits, so that fp32 results are as good
 //                as fp32 arithmetic makes them (two parts leave 1.6e-6 of the result; the third product
 //                is hidden behind the stream).
-constexpr int kInstGeneral = 0, kInstUniform = 1, kInstScores = 2;
+//  kInstFold     the tails of requests that share prefixes: it skips the shared pages and folds the partial
+//                results over the prefix (shared_prefix.cu) into each row before it is stored.  Three parts
+//                of P like kInstScores.
+constexpr int kInstGeneral = 0, kInstUniform = 1, kInstScores = 2, kInstFold = 3;
 template <int D, int G, int kInst>
 __global__ void __launch_bounds__(TmaCfg<D>::kThreads, 2)
 splitkv_tma_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtensorMap kmap,
@@ -264,7 +268,9 @@ splitkv_tma_kernel(const __grid_constant__ AttnParams p, const __grid_constant__
             r.first = item_first;
             if (item_first) { r.item = it; r.take = take; }
             item_first = false;
-            blk = lane < r.n ? __ldg(p.block_table + (size_t)it.b * p.max_blocks_per_seq + item_logical_page(it, v + lane)) : 0;
+            const int32_t* table = p.block_table + (size_t)it.b * p.max_blocks_per_seq;
+            if constexpr (kInst == kInstFold) table += __ldcg(p.page_shift + it.b);
+            blk = lane < r.n ? __ldg(table + item_logical_page(it, v + lane)) : 0;
             v += r.n;
             if (v >= nv) {
                 x += take;
@@ -344,7 +350,44 @@ splitkv_tma_kernel(const __grid_constant__ AttnParams p, const __grid_constant__
         // 128-bit loads and stores the result straight from the fragment.
         const int hrow = lane >> 2, qc = (lane & 3) * 2;
         const float kLn2 = 0.6931471805599453f;
-        auto store_final = [&](const Item& it, const float (&o)[D / 16][4], const float4& ml) {
+        // folds the partial results over the request's shared prefix into the row, chunk after chunk
+        auto fold_shared = [&](const Item& it, float (&o)[D / 16][4], float4& ml) {
+            const SharedDesc& sd = *p.shared;
+            const int tiles = __ldcg(&sd.rows[it.b].tiles);
+            if (tiles == 0) return;
+            const int gl = __ldcg(&sd.gated_index[it.layer]), nseg = __ldcg(&sd.nseg);
+            const long long total = __ldcg(&sd.total);
+            const long long u0 = ((long long)gl * p.num_kv_heads + it.g) * __ldcg(&sd.t1) + __ldcg(&sd.rows[it.b].unit);
+            const int j0 = (int)(((u0 + 1) * nseg - 1) / total);            // the spans of its first and last tile
+            const int j1 = (int)(((u0 + tiles) * nseg - 1) / total);
+            const size_t own = ((size_t)gl * p.batch + it.b) * p.num_q_heads + it.g * G;
+            const size_t ext = p.shared_ext_row0 + __ldcg(&sd.rows[it.b].row);
+            for (int j = j0; j <= j1; ++j) {
+                const size_t row = j == j0 ? own : ext + (size_t)j * 256;
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    if (qc + e >= G) continue;
+                    const float2 pm = __ldcg(p.shared_ml + row + qc + e);
+                    const float* src = p.shared_o + (row + qc + e) * D + hrow;
+                    float v[D / 8];
+#pragma unroll
+                    for (int n = 0; n < D / 8; ++n) v[n] = __ldcg(src + n * 8);
+                    float& mm = e ? ml.z : ml.x;
+                    float& ll = e ? ml.w : ml.y;
+                    const float mn = fmaxf(mm, pm.x), mu = mn == -INFINITY ? 0.f : mn;
+                    const float a = ex2(mm - mu), c = ex2(pm.x - mu);
+                    mm = mn;
+                    ll = ll * a + pm.y * c;
+#pragma unroll
+                    for (int n = 0; n < D / 16; ++n) {
+                        o[n][e] = o[n][e] * a + v[2 * n] * c;
+                        o[n][2 + e] = o[n][2 + e] * a + v[2 * n + 1] * c;
+                    }
+                }
+            }
+        };
+        auto store_final = [&](const Item& it, float (&o)[D / 16][4], float4 ml) {
+            if constexpr (kInst == kInstFold) fold_shared(it, o, ml);
             // remainder mode: the Local lse is read by every lane of a head before any lane replaces it
             float l_old2[2] = {0.f, 0.f};
             if (p.mode == 2) {
@@ -813,10 +856,10 @@ bool tma_variant_supported(int head_dim, int64_t layer_stride, int64_t block_str
 }
 
 // 5-D view of a paged cache: (d within a 64-wide slab, slot, slab, kv head, block); one box = one
-// page of one head.  The block extent is a loose bound: the kernel only reads blocks that the
-// block table names.
+// page of one head (box_slabs = 0), or of that many slabs of it.  The block extent is a loose bound:
+// the kernel only reads blocks that the block table names.
 bool encode_kv_map(void* out_map, const void* base, int head_dim, int num_kv_heads, int64_t token_stride,
-                   int64_t head_stride, int64_t block_stride, int64_t num_blocks_bound)
+                   int64_t head_stride, int64_t block_stride, int64_t num_blocks_bound, int box_slabs)
 {
     EncodeTiledFn fn = encode_fn();
     if (!fn) return false;
@@ -824,7 +867,7 @@ bool encode_kv_map(void* out_map, const void* base, int head_dim, int num_kv_hea
                           (cuuint64_t)num_blocks_bound};
     cuuint64_t strides[4] = {(cuuint64_t)token_stride * 2, 128, (cuuint64_t)head_stride * 2,
                              (cuuint64_t)block_stride * 2};
-    cuuint32_t box[5] = {64, (cuuint32_t)kPage, (cuuint32_t)(head_dim / 64), 1, 1};
+    cuuint32_t box[5] = {64, (cuuint32_t)kPage, (cuuint32_t)(box_slabs ? box_slabs : head_dim / 64), 1, 1};
     cuuint32_t estr[5] = {1, 1, 1, 1, 1};
     CUresult r = fn(reinterpret_cast<CUtensorMap*>(out_map), CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5,
                     const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
@@ -853,6 +896,7 @@ static cudaError_t launch_tma_t(const AttnParams& p, const void* kmap, const voi
         cudaError_t e = prepare_tma_t<D, G, kInstGeneral>();
         if (e == cudaSuccess) e = prepare_tma_t<D, G, kInstUniform>();
         if (e == cudaSuccess) e = prepare_tma_t<D, G, kInstScores>();
+        if (e == cudaSuccess) e = prepare_tma_t<D, G, kInstFold>();
         if (e != cudaSuccess) return e;
         attr_set = true;
     }
@@ -861,6 +905,8 @@ static cudaError_t launch_tma_t(const AttnParams& p, const void* kmap, const voi
     const dim3 g(grid), t(TmaCfg<D>::kThreads);
     if (p.score_rows)
         return launch_ex(splitkv_tma_kernel<D, G, kInstScores>, g, t, TmaCfg<D>::kSmemBytes, st, pdl, p, km, vm, blocks_per_layer);
+    if (p.shared)
+        return launch_ex(splitkv_tma_kernel<D, G, kInstFold>, g, t, TmaCfg<D>::kSmemBytes, st, pdl, p, km, vm, blocks_per_layer);
     if (p.uniform_hint && !p.direct_hint)
         return launch_ex(splitkv_tma_kernel<D, G, kInstUniform>, g, t, TmaCfg<D>::kSmemBytes, st, pdl, p, km, vm, blocks_per_layer);
     return launch_ex(splitkv_tma_kernel<D, G, kInstGeneral>, g, t, TmaCfg<D>::kSmemBytes, st, pdl, p, km, vm, blocks_per_layer);
