@@ -144,6 +144,8 @@ bool refresh_map(oda_ctx* c, void* map, const void** base, const void* cache, in
     return true;
 }
 
+constexpr int kTailMinSpan = 8;   // pages of a span of tails (short units beside which the merge weighs little)
+
 // what the passes that build on the gated Full pass add to its launch
 struct AttnExtra {
     float* score_rows = nullptr;   // weighted pass: see AttnParams
@@ -226,7 +228,8 @@ oda_status_t launch_attention(oda_ctx* c, int mode, int lb, int le, int batch, c
     p.done_counter = reinterpret_cast<int32_t*>(c->ws + c->lay.status + 128);
     p.exit_counter = reinterpret_cast<int32_t*>(c->ws + c->lay.status + 192);
     p.num_sms = c->num_sms;
-    if (c->calibrating) p.sm_stats = reinterpret_cast<unsigned long long*>(c->ws + c->lay.sm_bytes);
+    if (c->calibrating && !(extra && extra->shared))  // (tails wait for the other kernel: no rates to learn)
+        p.sm_stats = reinterpret_cast<unsigned long long*>(c->ws + c->lay.sm_bytes);
     if (c->calibrated) {
         p.cum_share = reinterpret_cast<const uint16_t*>(c->ws + c->lay.cum_share);
         p.sm_claims = reinterpret_cast<int32_t*>(c->ws + c->lay.sm_claims);
@@ -236,12 +239,12 @@ oda_status_t launch_attention(oda_ctx* c, int mode, int lb, int le, int batch, c
         p.score_rows = extra->score_rows;
         p.score_ml = extra->score_ml;
         if (const SharedParams* sp = extra->shared) {
-            p.page_shift = sp->page_shift;
-            p.seq_lens = sp->tail_lens;
-            p.shared = sp->desc;
-            p.shared_o = sp->part_o;
-            p.shared_ml = sp->part_ml;
-            p.shared_ext_row0 = sp->ext_row0;
+            p.group_start = sp->group_start;
+            p.group_prefix = sp->group_prefix;
+            p.num_groups = sp->num_groups;
+            p.tail_o = sp->tail_o;
+            p.tail_ml = sp->tail_ml;
+            p.min_span_pages = kTailMinSpan;
         }
     }
     // A Local call over few layers cannot fill the usual grid: the window bounds its pages whatever
@@ -1227,7 +1230,7 @@ oda_status_t oda_evict(oda_ctx_t* c, int32_t batch, float* weights, void* k, voi
 }
 
 struct SharedScratch {
-    size_t desc, shift, tails, ml, o, total, ext_row0;
+    size_t desc, ml, o, tail_ml, tail_o, total, ext_row0;
 };
 static SharedScratch shared_scratch(const oda_ctx* c)
 {
@@ -1236,12 +1239,12 @@ static SharedScratch shared_scratch(const oda_ctx* c)
     size_t off = 0;
     auto take = [&](size_t bytes) { size_t o = off; off = align_up(off + bytes); return o; };
     w.desc = take(sizeof(SharedDesc));
-    w.shift = take(kMaxBatch * sizeof(int32_t));
-    w.tails = take(kMaxBatch * sizeof(int32_t));
     w.ext_row0 = (size_t)f.num_layers * f.max_batch * f.num_q_heads;
     const size_t rows = w.ext_row0 + (size_t)c->num_sms * 256;  // and the rows of one block for every span
     w.ml = take(rows * sizeof(float2));
     w.o = take(rows * f.head_dim * sizeof(float));
+    w.tail_ml = take(w.ext_row0 * sizeof(float2));
+    w.tail_o = take(w.ext_row0 * f.head_dim * sizeof(float));
     w.total = off;
     return w;
 }
@@ -1262,6 +1265,8 @@ oda_status_t oda_full_decode_shared(oda_ctx_t* c, int32_t lb, int32_t le, int32_
         return fail(c, ODA_ERR_UNSUPPORTED, "the shared-prefix Full pass exists in the TMA variant only");
     if (!scratch || (reinterpret_cast<uintptr_t>(scratch) % kAlign) != 0 || scratch_bytes < oda_full_decode_shared_scratch_bytes(c))
         return fail(c, ODA_ERR_WORKSPACE, "scratch is null, misaligned or smaller than oda_full_decode_shared_scratch_bytes()");
+    if (num_groups == 0)  // nobody shares anything
+        return launch_attention(c, 1, lb, le, batch, q, k, v, bt, sl, flags, out, lse, static_cast<cudaStream_t>(stream));
     const oda_config_t& f = c->cfg;
     const SharedScratch w = shared_scratch(c);
     char* base = static_cast<char*>(scratch);
@@ -1281,10 +1286,13 @@ oda_status_t oda_full_decode_shared(oda_ctx_t* c, int32_t lb, int32_t le, int32_
     p.group_prefix = group_prefix;
     p.status = reinterpret_cast<int32_t*>(c->ws + c->lay.status);
     p.desc = reinterpret_cast<SharedDesc*>(base + w.desc);
-    p.page_shift = reinterpret_cast<int32_t*>(base + w.shift);
-    p.tail_lens = reinterpret_cast<int32_t*>(base + w.tails);
     p.part_ml = reinterpret_cast<float2*>(base + w.ml);
     p.part_o = reinterpret_cast<float*>(base + w.o);
+    p.tail_ml = reinterpret_cast<float2*>(base + w.tail_ml);
+    p.tail_o = reinterpret_cast<float*>(base + w.tail_o);
+    p.out = out;
+    p.lse = lse;
+    p.layer_begin = lb;
     p.ext_row0 = w.ext_row0;
     p.batch = batch;
     p.num_groups = num_groups;
@@ -1302,7 +1310,12 @@ oda_status_t oda_full_decode_shared(oda_ctx_t* c, int32_t lb, int32_t le, int32_
     c->launches += 1;
     AttnExtra x;
     x.shared = &p;
-    return launch_attention(c, 1, lb, le, batch, q, k, v, bt, sl, flags, out, lse, st, nullptr, nullptr, nullptr, &x);
+    s = launch_attention(c, 1, lb, le, batch, q, k, v, bt, sl, flags, out, lse, st, nullptr, nullptr, nullptr, &x);
+    if (s != ODA_OK) return s;
+    e = launch_shared_join(p, f.head_dim, f.out_dtype != 0, st, c->use_pdl);
+    if (e != cudaSuccess) return cuda_fail(c, e, "shared-prefix join launch");
+    c->launches += 1;
+    return ODA_OK;
 }
 
 }  // extern "C"

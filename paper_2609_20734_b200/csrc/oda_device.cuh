@@ -23,8 +23,6 @@ struct LayerInfo {  // one per layer, in the workspace
     int32_t window, sinks, gated, kv_index, cls, pad0, pad1, pad2;
 };
 
-struct SharedDesc;
-
 struct AttnParams {
     const __nv_bfloat16* q;
     const __nv_bfloat16* k;
@@ -74,13 +72,13 @@ struct AttnParams {
     // what turns them into weights once a row is finished.  Layers count from layer_begin.
     float* score_rows;          // [layers][batch][kv heads][max positions][group]
     float2* score_ml;           // [layers][batch][q heads]: (m, 1 / l), weight = 2^(logit - m) / l
-    // Full pass over the tails of requests that share prefixes (the fold instance): pages of the table that a
-    // request skips, and where the partial results over its prefix are (shared_prefix.cuh)
-    const int32_t* page_shift;  // [batch]
-    const SharedDesc* shared;
-    const float* shared_o;
-    const float2* shared_ml;
-    size_t shared_ext_row0;
+    // Full pass over the tails of requests that share prefixes (the tail instance, shared_prefix.cuh): the groups,
+    // and where the rows go as partial results.  Layers count from layer_begin.
+    const int32_t* group_start;
+    const int32_t* group_prefix;
+    int32_t num_groups;
+    float* tail_o;              // [layers][batch][q heads][D], unnormalised
+    float2* tail_ml;            // [layers][batch][q heads]: (m in log2 units, l)
 };
 
 // Programmatic dependent launch: a kernel launched with the stream-serialisation attribute may
@@ -196,7 +194,8 @@ __device__ __forceinline__ bool unit_aligned_shape(long long total, int umin, in
     return (long long)umin * nseg >= total && (long long)umax * nseg <= 4 * total && 150ll * umax <= total + 4200;
 }
 
-__device__ inline void build_plan(const AttnParams& p, Plan& pl)
+// `tails` (shared memory): lengths to plan with instead of seq_lens.
+__device__ inline void build_plan(const AttnParams& p, Plan& pl, const int32_t* tails = nullptr)
 {
     const int tid = threadIdx.x, nth = blockDim.x;
     const int B = p.batch;
@@ -257,7 +256,7 @@ __device__ inline void build_plan(const AttnParams& p, Plan& pl)
     }
     // issue every global load of the plan before using any of them: one memory latency, not three
     const bool has_b = tid < B;  // blockDim.x >= kMaxBatch
-    const int t_raw = has_b ? p.seq_lens[tid] : 1;
+    const int t_raw = has_b ? (tails ? tails[tid] : p.seq_lens[tid]) : 1;
     const int fl_raw = (has_b && p.mode != 0) ? p.flags[tid] : 1;
     LayerInfo li0, li1;
     li0.cls = li0.kv_index = li1.cls = li1.kv_index = 0;

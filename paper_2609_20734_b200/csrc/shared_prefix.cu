@@ -1,28 +1,37 @@
 // Attention of many requests over a prefix that they share, on the 5th-generation tensor cores.
 //
-// The gated Full pass over shared prefixes is two launches.  This kernel does the shared part: for every (gated
-// layer, kv head, group of requests) the query heads of all flagged requests of the group are the rows of one
+// The gated Full pass over shared prefixes is three launches.  shared_prefix_kernel does the shared part: for every
+// (gated layer, kv head, group of requests) the query heads of all flagged requests of the group are the rows of one
 // matrix Q, and
 //     S = Q K^T,  P = 2^(scale S - m),  O = P V,  l = P 1
-// runs over the prefix once.  What is left of each request -- its own tail of positions -- goes to the split-KV
-// kernel, whose epilogue folds the partial results of this kernel in (SharedDesc says where they are).
+// runs over the prefix once.  What is left of each request -- its own tail of positions -- is the split-KV kernel's,
+// which runs beside this one where there is room, and shared_join_kernel adds both up:
+//     out = sum_i 2^(m_i - M) O_i / sum_i 2^(m_i - M) l_i
+// over the tail and the chunks of the prefix, in that order.
 //
 // Only whole pages are shared (a page that the prefix ends in is read through each request's own table row), and
-// every request keeps at least one position of its own, so the second kernel visits every flagged request.
+// every request keeps at least one position of its own, so the tail kernel leaves a row of every flagged request.
 //
 // Work: rows are cut into blocks of 256 (two 128-row MMA tiles), prefixes into tiles of kTokens positions; all
 // (layer, kv head, group, row block, tile) lie on one axis that is cut into equal spans, one per CTA (one CTA per SM).
 // A unit that a span boundary cuts leaves several partials; nobody waits for another CTA.
 //
-// A CTA: two softmax warpgroups ("streams"), one producer warp (TMA), one MMA warp (one thread issues).  With more than
+// A CTA: two softmax warpgroups ("streams"), an MMA warp for each (one thread issues) and a producer warp (TMA).  With more than
 // 128 rows the streams are the two row tiles and both use every K/V tile; with fewer, both have the same rows and take
 // the tiles in turn (stream 0 the even ones), and their results are joined through TMEM at the end.  Either way one
 // stream's softmax runs while the tensor core works for the other.  TMEM: S of both streams (kTokens columns each; P
 // replaces S in place as bf16) and O of both streams (D columns each).
 //
-// P in bf16: kTerms parts of 8 bits each.  Three for fp32 results (24 bits: nothing is lost against fp32 arithmetic);
-// for bf16 results see launch_shared_prefix.
+// Two forms of the kernel, chosen by the most rows that a kv head can have in the call (batch x group):
+//   narrow (<= 128 rows): bound by the stream of K and V.  Tiles of 64 positions, one copy of Q, and the rest of shared
+//     memory as a ring: what waits for its softmax is small, what is on its way large.
+//   wide: bound by the products and the exponentials.  Tiles of 128 positions and 2 x 128 rows.
+//
+// P in bf16 is kTerms parts of 8 bits each.  fp32 results take three (24 bits: nothing is lost against fp32
+// arithmetic), bf16 results two in the narrow form, where the second product hides behind the stream.
 #include <cuda.h>
+
+#include <algorithm>
 
 #include "launch_ex.cuh"
 #include "mbar.cuh"
@@ -32,30 +41,27 @@
 
 namespace oda {
 
-constexpr int kShThreads = 320;
 constexpr int kShRows = 128;       // rows of one MMA tile
 constexpr int kShMinTiles = 2;     // a CTA is not given fewer tiles than this (unless there are fewer)
 
-template <int D, int kTerms>
+template <int D, int kTerms, bool kWide>
 struct ShCfg {
-    static constexpr int kTokens = kTerms == 3 ? 64 : 128;  // S (and three parts of P) of two streams beside O in 512 columns
+    static constexpr int kTokens = kWide && kTerms < 3 ? 128 : 64;
     static constexpr int kTilePages = kTokens / kPage;
     static constexpr int kSlotBytes = kTokens * D * 2;      // K or V of one tile
-    static constexpr int kSlots = 131072 / kSlotBytes > 16 ? 16 : 131072 / kSlotBytes;
+    static constexpr int kRing = kWide ? 131072 : 180224;
+    static constexpr int kSlots = kRing / kSlotBytes > 16 ? 16 : kRing / kSlotBytes;
     static constexpr int kQBytes = kShRows * D * 2;
-    static constexpr int kSpCols = kTerms == 3 ? 96 : kTokens;  // columns of one stream's S and P
+    static constexpr int kQTiles = kWide ? 2 : 1;
+    static constexpr int kSpCols = kTokens / 2 * kTerms > kTokens ? kTokens / 2 * kTerms : kTokens;  // one stream's S, then P
     static constexpr int kO0 = 2 * kSpCols;                 // first column of stream 0's O
+    static constexpr int kRowBlock = kWide ? 256 : 128;     // rows of a unit
     static_assert(2 * kSpCols + 2 * D <= 512, "TMEM");
 };
 
 struct ShPlan {
-    int32_t t[kMaxBatch];            // lengths, clamped to the table
-    int32_t gs[kMaxBatch + 1];
+    SharedGroups g;
     int32_t off[kMaxBatch + 1];      // first tile of each group within one (layer, kv head)
-    int32_t pages[kMaxBatch];        // shared pages of the group (0: shares nothing)
-    uint8_t members[kMaxBatch];      // flagged ones of each group
-    uint8_t act[kMaxBatch];
-    uint8_t list[kMaxBatch];         // flagged requests, those of group i from gs[i] on
     int32_t t1, total, nseg;
 };
 
@@ -81,21 +87,29 @@ __device__ __forceinline__ void tc_commit(uint32_t bar)
 {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
-// D[128 x N] (+)= A B with A and B in shared memory
-__device__ __forceinline__ void tc_mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool acc)
+// D[128 x N] (+)= A B with A and B in shared memory: low words of the descriptors (address and lbo); see smem_lo
+__device__ __forceinline__ void tc_mma_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t hi, uint32_t idesc, bool acc)
 {
     asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-        ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)acc) : "memory");
+        "{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\tsetp.ne.u32 p, %5, 0;\n\t"
+        "mov.b64 da, {%1, %3};\n\tmov.b64 db, {%2, %3};\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %4, p;\n\t}"
+        ::"r"(d), "r"(a), "r"(b), "r"(hi), "r"(idesc), "r"((uint32_t)acc) : "memory");
 }
 // the same with A in TMEM
-__device__ __forceinline__ void tc_mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool acc)
+__device__ __forceinline__ void tc_mma_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t hi, uint32_t idesc, bool acc)
 {
     asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
-        ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)acc) : "memory");
+        "{\n\t.reg .pred p;\n\t.reg .b64 db;\n\tsetp.ne.u32 p, %5, 0;\n\t"
+        "mov.b64 db, {%2, %3};\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %4, p;\n\t}"
+        ::"r"(d), "r"(a), "r"(b), "r"(hi), "r"(idesc), "r"((uint32_t)acc) : "memory");
+}
+__device__ __forceinline__ bool elect_one()
+{
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+    return r != 0;
 }
 __device__ __forceinline__ void tc_ld32(uint32_t addr, float* v)
 {
@@ -129,14 +143,11 @@ __device__ __forceinline__ void tc_st16(uint32_t addr, const uint32_t* r)
           "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
         : "memory");
 }
-// Shared-memory operand, 128-byte swizzle.  K-major (Q, K): rows of 128 bytes, groups of 8 rows `sbo` bytes apart.
-// MN-major (V): 64 columns of a position are one 128-byte row, groups of 8 positions `sbo` apart, the next 64
-// columns `lbo` away.
-__device__ __forceinline__ uint64_t smem_desc(uint32_t addr, uint32_t lbo, uint32_t sbo)
-{
-    return (uint64_t)((addr & 0x3ffffu) >> 4) | ((uint64_t)(lbo >> 4) << 16) | ((uint64_t)(sbo >> 4) << 32) |
-           (1ull << 46) | (2ull << 61);
-}
+// Shared-memory operand, 128-byte swizzle.  K-major (Q, K): rows of 128 bytes, groups of 8 rows 1024 bytes apart (lbo
+// not used).  MN-major (V): 64 columns of a position are one 128-byte row, groups of 8 positions 1024 bytes apart, the
+// next 64 columns `lbo` away.
+__device__ __forceinline__ uint32_t smem_lo(uint32_t addr, uint32_t lbo) { return ((addr & 0x3ffffu) >> 4) | ((lbo >> 4) << 16); }
+constexpr uint32_t kDescHi = (1024u >> 4) | (1u << 14) | (2u << 29);
 constexpr uint32_t idesc_bf16(int n, bool b_mn_major)  // M = 128, fp32 accumulators
 {
     return (1u << 4) | (1u << 7) | (1u << 10) | (b_mn_major ? 1u << 16 : 0u) | ((uint32_t)(n / 8) << 17) | ((128u / 16) << 24);
@@ -145,6 +156,31 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi)
 {
     uint32_t r;
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+// two fp32 values in one 64-bit register: one instruction for both
+__device__ __forceinline__ uint64_t pair(float x, float y)
+{
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
+    return r;
+}
+__device__ __forceinline__ float2 unpair(uint64_t v)
+{
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+    return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c)
+{
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b)
+{
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
     return r;
 }
 __device__ __forceinline__ void tma_box(uint32_t dst, const CUtensorMap* map, uint32_t bar, int slab, int head, int block, uint64_t policy)
@@ -162,49 +198,20 @@ __device__ __forceinline__ bool warp_wait(const uint64_t* bar, uint32_t parity, 
 }
 
 // ------------------------------------------------------------------ plan
-// The same in every CTA, from the device-resident lengths, flags and groups.  CTA 0 also writes the descriptor that
-// the second kernel works from, and reports what is wrong with the lengths and groups.
-template <int TP>
+// The same in every CTA.  CTA 0 also writes the descriptor that the second kernel works from, and reports what is
+// wrong with the lengths and groups.
+template <int TP, int kRowBlock>
 __device__ __forceinline__ void shared_plan(const SharedParams& p, ShPlan& pl)
 {
     const int tid = threadIdx.x, B = p.batch, NG = p.num_groups;
-    const int cap = p.max_blocks_per_seq * kPage;
-    int t_raw = 0, fl = 0;
-    if (tid < B) {
-        t_raw = p.seq_lens[tid];
-        fl = p.flags[tid];
-        pl.t[tid] = min(t_raw, cap);
-        pl.act[tid] = fl && t_raw >= 1;
-        if (fl && t_raw > cap && blockIdx.x == 0) atomicOr(p.status, kStatusBadSeqLen);
-    }
-    if (tid <= NG && NG > 0) pl.gs[tid] = p.group_start[tid];
-    __syncthreads();
-    if (tid < NG) {
-        const int s = pl.gs[tid], e = pl.gs[tid + 1];
-        bool ok = s >= 0 && e >= s && e <= B;
-        for (int k = 0; k < tid; ++k) ok = ok && pl.gs[k] <= s;  // nobody belongs to two groups
-        int n = 0, least = 0x7fffffff;
-        if (ok) {
-            for (int b = s; b < e; ++b)
-                if (pl.act[b]) {
-                    pl.list[s + n++] = (uint8_t)b;
-                    least = min(least, pl.t[b]);
-                }
-        } else if (blockIdx.x == 0) {
-            atomicOr(p.status, kStatusBadGroup);
-        }
-        // a lone request shares with nobody: its whole history is the second kernel's
-        const int shared = n >= 2 ? min(p.group_prefix[tid], least - 1) : 0;
-        pl.pages[tid] = shared > 0 ? shared / kPage : 0;
-        pl.members[tid] = (uint8_t)n;
-    }
-    __syncthreads();
+    SharedGroups& g = pl.g;
+    shared_groups(g, B, p.max_blocks_per_seq, p.seq_lens, p.flags, NG, p.group_start, p.group_prefix, p.status, blockIdx.x == 0);
     if (tid < 32) {
         long long carry = 0;
         for (int i0 = 0; i0 < NG; i0 += 32) {
             const int i = i0 + tid;
             long long own = 0;
-            if (i < NG) own = (long long)((pl.members[i] * p.group + 255) / 256) * ((pl.pages[i] + TP - 1) / TP);
+            if (i < NG) own = (long long)((g.members[i] * p.group + kRowBlock - 1) / kRowBlock) * ((g.pages[i] + TP - 1) / TP);
             long long x = own;
             for (int o = 1; o < 32; o <<= 1) {
                 const long long y = __shfl_up_sync(0xffffffffu, x, o);
@@ -214,15 +221,13 @@ __device__ __forceinline__ void shared_plan(const SharedParams& p, ShPlan& pl)
             carry += __shfl_sync(0xffffffffu, x, 31);
         }
         if (tid == 0) {
-            long long total = carry * p.num_kv_heads * p.num_gated;
-            if (carry > 0x7fffffffll || total > 0x7fffffffll) {  // beyond a 32-bit axis: nothing is shared
-                if (blockIdx.x == 0) atomicOr(p.status, kStatusItemOverflow);
-                total = carry = 0;
-            }
-            pl.off[NG] = (int32_t)carry;
-            pl.t1 = (int32_t)carry;
-            pl.total = (int32_t)total;
-            pl.nseg = total > 0 ? (int)max(1ll, min((long long)gridDim.x, total / kShMinTiles)) : 0;
+            // (pages of a prefix fill 32-bit positions, so this ends below 2^31 in every cache that fits a device)
+            const long long total = carry * p.num_kv_heads * p.num_gated;
+            if (total > 0x7fffffffll) atomicOr(p.status, kStatusItemOverflow);
+            pl.off[NG] = (int32_t)min(carry, 0x7fffffffll);
+            pl.t1 = pl.off[NG];
+            pl.total = total > 0x7fffffffll ? 0 : (int32_t)total;
+            pl.nseg = pl.total > 0 ? (int)max(1ll, min((long long)gridDim.x, total / kShMinTiles)) : 0;
         }
     }
     __syncthreads();
@@ -230,35 +235,28 @@ __device__ __forceinline__ void shared_plan(const SharedParams& p, ShPlan& pl)
         SharedDesc& d = *p.desc;
         if (tid == 0) {
             d.t1 = pl.t1;
-            d.total = pl.total;
+            d.total = max(pl.total, 1);
             d.nseg = pl.nseg;
         }
-        for (int l = tid; l < p.num_gated; l += kShThreads) d.gated_index[p.layer[l]] = l;
+        for (int l = tid; l < p.num_gated; l += blockDim.x) d.gated_index[p.layer[l]] = l;
         if (tid < B) {
             SharedRow r;
-            r.unit = r.tiles = r.row = 0;
-            int shift = 0;
-            if (pl.total > 0 && pl.act[tid]) {
-                for (int i = 0; i < NG; ++i) {
-                    if (pl.pages[i] == 0 || tid < pl.gs[i] || tid >= pl.gs[i + 1]) continue;
-                    int rank = 0;
-                    for (int k = 0; k < pl.members[i]; ++k) rank += pl.list[pl.gs[i] + k] < tid;
-                    const int per = 256 / p.group, block = rank / per;
-                    r.tiles = (pl.pages[i] + TP - 1) / TP;
-                    r.unit = pl.off[i] + block * r.tiles;
-                    r.row = (rank - block * per) * p.group;
-                    shift = pl.pages[i];
-                }
+            r.unit = r.tiles = r.row = r.pad = 0;
+            const int i = shared_group_of(g, NG, tid);
+            if (i >= 0 && pl.total > 0) {
+                int rank = 0;
+                for (int k = 0; k < g.members[i]; ++k) rank += g.list[g.gs[i] + k] < tid;
+                const int per = kRowBlock / p.group, block = rank / per;
+                r.tiles = (g.pages[i] + TP - 1) / TP;
+                r.unit = pl.off[i] + block * r.tiles;
+                r.row = (rank - block * per) * p.group;
             }
             d.rows[tid] = r;
-            p.page_shift[tid] = shift;
-            // what the second kernel sees of the request (a length below 1 is left for it to report)
-            p.tail_lens[tid] = (t_raw < 1 ? t_raw : pl.t[tid]) - shift * kPage;
         }
     }
 }
 
-template <int TP>
+template <int TP, int kRowBlock>
 __device__ __forceinline__ ShItem shared_item(const SharedParams& p, const ShPlan& pl, int x, int x_end)
 {
     const int u = x / pl.t1, r = x - u * pl.t1;
@@ -271,26 +269,26 @@ __device__ __forceinline__ ShItem shared_item(const SharedParams& p, const ShPla
     it.gl = u / p.num_kv_heads;
     it.kvh = u - it.gl * p.num_kv_heads;
     it.group = lo;
-    it.pages = pl.pages[lo];
+    it.pages = pl.g.pages[lo];
     const int nt = (it.pages + TP - 1) / TP, r2 = r - pl.off[lo];
     const int block = r2 / nt;
     it.tile0 = r2 - block * nt;
     it.n = min(nt - it.tile0, x_end - x);
-    it.row0 = block * 256;
-    it.nrows = min(256, pl.members[lo] * p.group - it.row0);
+    it.row0 = block * kRowBlock;
+    it.nrows = min(kRowBlock, pl.g.members[lo] * p.group - it.row0);
     return it;
 }
 
-template <int D, int kTerms>
-__global__ void __launch_bounds__(kShThreads, 1)
+template <int D, int kTerms, bool kWide>
+__global__ void __launch_bounds__(384, 1)
 shared_prefix_kernel(const __grid_constant__ SharedParams p, const __grid_constant__ CUtensorMap kmap,
                      const __grid_constant__ CUtensorMap vmap)
 {
-    using C = ShCfg<D, kTerms>;
+    using C = ShCfg<D, kTerms, kWide>;
     constexpr int TP = C::kTilePages, TN = C::kTokens, kSlabs = D / 64;
     extern __shared__ __align__(1024) uint8_t smem[];
     uint8_t* qs = smem;
-    uint8_t* ring = smem + 2 * C::kQBytes;
+    uint8_t* ring = smem + C::kQTiles * C::kQBytes;
     ShPlan& pl = *reinterpret_cast<ShPlan*>(ring + C::kSlots * C::kSlotBytes);
     ShCtl& ctl = *reinterpret_cast<ShCtl*>(reinterpret_cast<uint8_t*>(&pl) + (sizeof(ShPlan) + 15) / 16 * 16);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -298,7 +296,7 @@ shared_prefix_kernel(const __grid_constant__ SharedParams p, const __grid_consta
     if (tid == 0) {
         for (int s = 0; s < C::kSlots; ++s) {
             mbar_init(smem_u32(&ctl.full[s]), 1);
-            mbar_init(smem_u32(&ctl.empty[s]), 1);
+            mbar_init(smem_u32(&ctl.empty[s]), kWide ? 2 : 1);
         }
         for (int s = 0; s < 2; ++s) {
             mbar_init(smem_u32(&ctl.s_full[s]), 1);
@@ -314,7 +312,7 @@ shared_prefix_kernel(const __grid_constant__ SharedParams p, const __grid_consta
         asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&vmap)) : "memory");
     }
     griddep_wait();
-    shared_plan<TP>(p, pl);  // begins and ends its phases with barriers
+    shared_plan<TP, C::kRowBlock>(p, pl);
     griddep_launch_dependents();
     const int span = (int)blockIdx.x;
     if (span >= pl.nseg) return;
@@ -328,6 +326,10 @@ shared_prefix_kernel(const __grid_constant__ SharedParams p, const __grid_consta
     const uint32_t tmem = ctl.tmem;
     const int x0 = (int)((long long)span * pl.total / pl.nseg), x1 = (int)((long long)(span + 1) * pl.total / pl.nseg);
 
+    // (wide form: 384 x 168 registers were launched with; the softmax warps take what the others do not need:
+    // 256 x 216 + 128 x 72)
+    if (warp >= 8) {
+    if constexpr (kWide) asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
     if (warp == 8) {
         // ============================ producer warp ============================
         const uint64_t once = 0x12F0000000000000ull;    // L2 evict-first: read by one row block
@@ -335,24 +337,29 @@ shared_prefix_kernel(const __grid_constant__ SharedParams p, const __grid_consta
         uint32_t cnt = 0;
         bool dead = false;
         for (int x = x0; x < x1 && !dead;) {
-            const ShItem it = shared_item<TP>(p, pl, x, x1);
+            const ShItem it = shared_item<TP, C::kRowBlock>(p, pl, x, x1);
             x += it.n;
-            const int ahead = it.nrows > kShRows ? 1 : 2;
-            const int lead = pl.list[pl.gs[it.group]];
+            const int ahead = kWide && it.nrows > kShRows ? 1 : 2;
+            const int lead = pl.g.list[pl.g.gs[it.group]];
             const int32_t* table = p.block_table + (size_t)lead * p.max_blocks_per_seq;
             const int first = it.tile0 * TP, last = min(it.pages, (it.tile0 + it.n) * TP);
             const int kv0 = p.kv_index[it.gl] * p.blocks_per_layer;
-            const uint64_t policy = pl.members[it.group] * p.group > 256 ? again : once;
-            // block ids of 32 pages from page `base` on, the lanes' own; K runs up to two tiles ahead of V
-            int base_k = -64, ids_k = 0, base_v = -64, ids_v = 0;
+            const uint64_t policy = pl.g.members[it.group] * p.group > C::kRowBlock ? again : once;
+            // block ids of 32 pages from page `base` on and of the 32 behind them, one per lane; K runs ahead of V
+            struct Ids { int base, now, next; } ids_k, ids_v;
+            auto fetch = [&](int pg) { return pg + lane < last ? __ldg(table + pg + lane) : 0; };
+            ids_k.base = ids_v.base = first;
+            ids_k.now = ids_v.now = fetch(first);
+            ids_k.next = ids_v.next = fetch(first + 32);
             auto load = [&](int tile, bool is_v) {
                 const int pg = first + tile * TP, np = min(TP, last - pg);
-                int& base = is_v ? base_v : base_k;
-                int& ids = is_v ? ids_v : ids_k;
-                if (pg - base >= 32) {
-                    base = pg;
-                    ids = pg + lane < last ? __ldg(table + pg + lane) : 0;
+                Ids& id = is_v ? ids_v : ids_k;
+                if (pg - id.base >= 32) {
+                    id.base += 32;
+                    id.now = id.next;
+                    id.next = fetch(id.base + 32);
                 }
+                const int base = id.base, ids = id.now;
                 const uint32_t s = cnt % C::kSlots, ph = (cnt / C::kSlots) & 1;
                 if (!warp_wait(&ctl.empty[s], ph ^ 1, abort_flag, p.status)) return false;
                 const uint32_t bar = smem_u32(&ctl.full[s]);
@@ -383,109 +390,108 @@ shared_prefix_kernel(const __grid_constant__ SharedParams p, const __grid_consta
             const uint32_t c2 = cnt - 1 - k;
             if (!warp_wait(&ctl.empty[c2 % C::kSlots], (c2 / C::kSlots) & 1, abort_flag, p.status)) break;
         }
-    } else if (warp == 9) {
-        // ============================ MMA warp (one thread) ============================
-        if (lane == 0) {
-            constexpr uint32_t idesc_s = idesc_bf16(TN, false), idesc_o = idesc_bf16(D, true);
-            uint32_t cnt = 0, nq[2] = {0, 0}, np_[2] = {0, 0};
-            bool ok = true;
-            auto acquire = [&]() {  // next slot of the ring, in the producer's order
-                const uint32_t s = cnt % C::kSlots, ph = (cnt / C::kSlots) & 1;
-                ++cnt;
-                ok = mbar_wait(smem_u32(&ctl.full[s]), ph, abort_flag, p.status);
-                tc_fence_after();
-                return s;
+    } else if (warp < 11) {
+        // ============================ MMA warps: one per stream, one thread issues ============================
+        // (The loop is run by the whole warp on warp-uniform values, and descriptors differ by constants: a thread
+        // that computes them anew before each product issues one in 100 cycles, slower than they run.  One warp for
+        // both streams spent 1470 cycles on a tile of 64 positions, most of them on its barriers.)
+        const int s = warp - 9;
+        constexpr uint32_t idesc_s = idesc_bf16(TN, false), idesc_o = idesc_bf16(D, true);
+        const bool leader = elect_one();
+        const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
+        const uint32_t ts = tm + s * C::kSpCols, to = tm + C::kO0 + s * D;  // S, then P; O
+        const uint32_t q_lo = smem_lo(smem_u32(qs), 16) + (kWide ? s : 0) * (C::kQBytes >> 4);
+        const uint32_t k_lo = smem_lo(smem_u32(ring), 16), v_lo = smem_lo(smem_u32(ring), 2048);
+        uint32_t base = 0;               // tensors in the ring before the item
+        uint32_t nq = 0, np = 0;
+        bool ok = true;
+        for (int x = x0; x < x1 && ok;) {
+            const ShItem item = shared_item<TP, C::kRowBlock>(p, pl, x, x1);
+            x += item.n;
+            const int n = __shfl_sync(0xffffffffu, item.n, 0);
+            const bool dual = kWide && __shfl_sync(0xffffffffu, item.nrows, 0) > kShRows;
+            const int rest = __shfl_sync(0xffffffffu, item.pages - item.tile0 * TP, 0);  // pages from the item's first on
+            const int ahead = dual ? 1 : 2, lead = min(ahead, n);
+            // place of K_t and V_t in the producer's order: K_0 (K_1), then V_t, K_(t+ahead) in turn
+            auto place = [&](int t, bool is_v) {
+                if (!is_v && t < ahead) return base + t;
+                const int u = is_v ? t : t - ahead;                    // V_u is behind u V's and the K's that followed them
+                return base + lead + u + min(u, n - lead) + (is_v ? 0u : 1u);
             };
-            auto qk = [&](int s, uint32_t slot) {  // S of stream s, whole tile (columns past the last page are not used)
-                const uint32_t a = smem_u32(qs + s * C::kQBytes), b = smem_u32(ring + slot * C::kSlotBytes);
-#pragma unroll
-                for (int k = 0; k < D / 16; ++k)
-                    tc_mma_ss(tmem + s * C::kSpCols, smem_desc(a + (k >> 2) * (kShRows * 128) + (k & 3) * 32, 16, 1024),
-                              smem_desc(b + (k >> 2) * (TN * 128) + (k & 3) * 32, 16, 1024), idesc_s, k > 0);
-                tc_commit(smem_u32(&ctl.s_full[s]));
-            };
-            auto pv = [&](int s, uint32_t slot, int pages, bool first) {
-                ok = mbar_wait(smem_u32(&ctl.p_full[s]), np_[s]++ & 1, abort_flag, p.status);
-                if (!ok) return;
+            auto acquire = [&](uint32_t at) {
+                const uint32_t sl = at % C::kSlots;
+                ok = warp_wait(&ctl.full[sl], (at / C::kSlots) & 1, abort_flag, p.status);
                 tc_fence_after();
-                const uint32_t b = smem_u32(ring + slot * C::kSlotBytes);
-                for (int k = 0; k < pages; ++k) {  // a page is one K step of 16 positions
-                    const uint64_t bd = smem_desc(b + k * (kPage * D * 2), 2048, 1024);
+                return sl;
+            };
+            auto release = [&](uint32_t sl) {  // in the wide form a slot is free after two arrivals: one of each stream,
+                if (!leader) return;           // or both of the only one that reads it
+                tc_commit(smem_u32(&ctl.empty[sl]));
+                if (kWide && !dual) tc_commit(smem_u32(&ctl.empty[sl]));
+            };
+            auto qk = [&](uint32_t sl) {       // whole tile (columns past the last page are not used)
+                const uint32_t b = k_lo + sl * (C::kSlotBytes >> 4);
+                if (leader) {
 #pragma unroll
-                    for (int c = 0; c < kTerms; ++c)
-                        tc_mma_ts(tmem + C::kO0 + s * D, tmem + s * C::kSpCols + c * (TN / 2) + k * 8, bd, idesc_o,
-                                  !first || k > 0 || c > 0);
+                    for (int k = 0; k < D / 16; ++k)
+                        tc_mma_ss(ts, q_lo + (k >> 2) * (kShRows * 128 >> 4) + (k & 3) * 2, b + (k >> 2) * (TN * 128 >> 4) + (k & 3) * 2,
+                                  kDescHi, idesc_s, k > 0);
+                    tc_commit(smem_u32(&ctl.s_full[s]));
                 }
             };
-            auto wait_q = [&](int s) {
-                ok = mbar_wait(smem_u32(&ctl.q_full[s]), nq[s]++ & 1, abort_flag, p.status);
+            // narrow: one copy of Q, loaded by stream 0 for every item; wide: each stream's own, where it has a tile
+            if (!kWide || dual || s < n) {
+                ok = warp_wait(&ctl.q_full[kWide ? s : 0], nq++ & 1, abort_flag, p.status);
+                if (!ok) break;
                 tc_fence_after();
-            };
-            for (int x = x0; x < x1 && ok;) {
-                const ShItem it = shared_item<TP>(p, pl, x, x1);
-                x += it.n;
-                const int first = it.tile0 * TP;
-                auto pages_of = [&](int t) { return min(TP, it.pages - first - t * TP); };
-                if (it.nrows > kShRows) {
-                    wait_q(0);
-                    if (ok) wait_q(1);
-                    uint32_t ks = ok ? acquire() : 0;
+            }
+            if (dual || s < n) {
+                const int step = dual ? 1 : 2, t0 = dual ? 0 : s;
+                uint32_t ks = acquire(place(t0, false));
+                if (!ok) break;
+                qk(ks);
+                release(ks);
+                for (int t = t0; t < n; t += step) {
+                    const uint32_t vs = acquire(place(t, true));
                     if (!ok) break;
-                    qk(0, ks);
-                    qk(1, ks);
-                    tc_commit(smem_u32(&ctl.empty[ks]));
-                    for (int t = 0; t < it.n; ++t) {
-                        const uint32_t vs = acquire();
+                    const bool more = t + step < n;
+                    if (more) {                // the next K is usually there: its barrier is looked at ahead of the products
+                        ks = acquire(place(t + step, false));
                         if (!ok) break;
-                        const bool more = t + 1 < it.n;
-                        pv(0, vs, pages_of(t), t == 0);
-                        if (!ok) break;
-                        if (more) {
-                            ks = acquire();
-                            if (!ok) break;
-                            qk(0, ks);
-                        } else {
-                            tc_commit(smem_u32(&ctl.o_full[0]));
-                        }
-                        pv(1, vs, pages_of(t), t == 0);
-                        if (!ok) break;
-                        tc_commit(smem_u32(&ctl.empty[vs]));
-                        if (more) {
-                            qk(1, ks);
-                            tc_commit(smem_u32(&ctl.empty[ks]));
-                        } else {
-                            tc_commit(smem_u32(&ctl.o_full[1]));
-                        }
                     }
-                } else {
-                    for (int t = 0; t < min(2, it.n) && ok; ++t) {
-                        wait_q(t);
-                        const uint32_t ks = ok ? acquire() : 0;
-                        if (!ok) break;
-                        qk(t, ks);
-                        tc_commit(smem_u32(&ctl.empty[ks]));
-                    }
-                    for (int t = 0; t < it.n && ok; ++t) {
-                        const int s = t & 1;
-                        const uint32_t vs = acquire();
-                        if (!ok) break;
-                        pv(s, vs, pages_of(t), t < 2);
-                        if (!ok) break;
-                        tc_commit(smem_u32(&ctl.empty[vs]));
-                        if (t + 2 < it.n) {
-                            const uint32_t ks = acquire();
-                            if (!ok) break;
-                            qk(s, ks);
-                            tc_commit(smem_u32(&ctl.empty[ks]));
+                    ok = warp_wait(&ctl.p_full[s], np++ & 1, abort_flag, p.status);
+                    if (!ok) break;
+                    tc_fence_after();
+                    const int pages = min(TP, rest - t * TP);
+                    const bool first = t == t0;
+                    const uint32_t b = v_lo + vs * (C::kSlotBytes >> 4);
+                    if (leader) {              // a page is one K step of 16 positions
+                        if (pages == TP) {
+#pragma unroll
+                            for (int k = 0; k < TP; ++k)
+#pragma unroll
+                                for (int c = 0; c < kTerms; ++c)
+                                    tc_mma_ts(to, ts + c * (TN / 2) + k * 8, b + k * (kPage * D * 2 >> 4), kDescHi, idesc_o, !first || k + c > 0);
                         } else {
-                            tc_commit(smem_u32(&ctl.o_full[s]));
+                            for (int k = 0; k < pages; ++k)
+#pragma unroll
+                                for (int c = 0; c < kTerms; ++c)
+                                    tc_mma_ts(to, ts + c * (TN / 2) + k * 8, b + k * (kPage * D * 2 >> 4), kDescHi, idesc_o, !first || k + c > 0);
                         }
                     }
+                    // (S of the next tile takes P's place: products of one thread run in order)
+                    if (more) qk(ks);
+                    release(vs);
+                    if (more) release(ks);
+                    if (!more && leader) tc_commit(smem_u32(&ctl.o_full[s]));
                 }
             }
+            base += 2 * n;
         }
         __syncwarp();
+    }
     } else {
+        if constexpr (kWide) asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
         // ============================ softmax warpgroups: one thread per row ============================
         const int s = warp >> 2;                     // stream
         const int tr = tid & (kShRows - 1);          // row of the tile = TMEM lane
@@ -495,9 +501,9 @@ shared_prefix_kernel(const __grid_constant__ SharedParams p, const __grid_consta
         uint32_t ns = 0, no = 0, nj = 0;
         bool ok = true;
         for (int x = x0; x < x1 && ok;) {
-            const ShItem it = shared_item<TP>(p, pl, x, x1);
+            const ShItem it = shared_item<TP, C::kRowBlock>(p, pl, x, x1);
             x += it.n;
-            const bool dual = it.nrows > kShRows;
+            const bool dual = kWide && it.nrows > kShRows;
             if (!dual && s == 1 && it.n == 1) continue;  // a lone tile: stream 0's
             const int row = dual ? s * kShRows + tr : tr;
             const bool valid = row < it.nrows;
@@ -506,8 +512,10 @@ shared_prefix_kernel(const __grid_constant__ SharedParams p, const __grid_consta
             int b = 0, head = 0;
             if (valid) {
                 const int r = it.row0 + row;
-                b = pl.list[pl.gs[it.group] + r / p.group];
+                b = pl.g.list[pl.g.gs[it.group] + r / p.group];
                 head = it.kvh * p.group + r % p.group;
+            }
+            if (valid && (kWide || s == 0)) {  // (narrow: one copy of Q, free again once both streams are joined)
                 const uint4* src = reinterpret_cast<const uint4*>(p.q + (((size_t)layer * p.batch + b) * p.num_q_heads + head) * D);
                 uint8_t* dst = qs + s * C::kQBytes + tr * 128;
                 uint4 v[D / 8];
@@ -517,9 +525,11 @@ shared_prefix_kernel(const __grid_constant__ SharedParams p, const __grid_consta
                 for (int c = 0; c < D / 8; ++c)
                     *reinterpret_cast<uint4*>(dst + (c >> 3) * (kShRows * 128) + (((c & 7) ^ (tr & 7)) << 4)) = v[c];
             }
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&ctl.q_full[s]));
+            if (kWide || s == 0) {
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&ctl.q_full[s]));
+            }
             float m = -INFINITY, l = 0.f;  // m in log2 units
             bool fresh = true;
             for (int t = dual ? 0 : s; t < it.n; t += dual ? 1 : 2) {
@@ -561,27 +571,30 @@ shared_prefix_kernel(const __grid_constant__ SharedParams p, const __grid_consta
                         }
                     }
                     const float mu = m == -INFINITY ? 0.f : m;
-                    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+                    const uint64_t scale2 = pair(scale, scale), mu2 = pair(-mu, -mu);
+                    uint64_t sum[2] = {0ull, 0ull};
 #pragma unroll
                     for (int c0 = 0; c0 < TN; c0 += 32) {
                         uint32_t part[kTerms][16];
 #pragma unroll
                         for (int e = 0; e < 32; e += 2) {
-                            float a = ex2(fmaf(v[c0 + e], scale, -mu)), c = ex2(fmaf(v[c0 + e + 1], scale, -mu));
-                            sum[e & 3] += a;
-                            sum[(e + 1) & 3] += c;
+                            const float2 z = unpair(fma2(pair(v[c0 + e], v[c0 + e + 1]), scale2, mu2));
+                            uint64_t w = pair(ex2(z.x), ex2(z.y));
+                            sum[(e >> 1) & 1] = add2(sum[(e >> 1) & 1], w);
 #pragma unroll
                             for (int k = 0; k < kTerms; ++k) {
-                                const uint32_t pk = pack2(a, c);
+                                const float2 a = unpair(w);
+                                const uint32_t pk = pack2(a.x, a.y);
                                 part[k][e / 2] = pk;
-                                a -= __uint_as_float(pk << 16);
-                                c -= __uint_as_float(pk & 0xffff0000u);
+                                if (k + 1 < kTerms)  // what is left after this part (exact)
+                                    w = add2(w, pair(-__uint_as_float(pk << 16), -__uint_as_float(pk & 0xffff0000u)));
                             }
                         }
 #pragma unroll
                         for (int k = 0; k < kTerms; ++k) tc_st16(sp + k * (TN / 2) + c0 / 2, part[k]);
                     }
-                    l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                    const float2 sums = unpair(add2(sum[0], sum[1]));
+                    l += sums.x + sums.y;
                     tc_wait_st();
                 }
                 tc_fence_before();
@@ -660,24 +673,121 @@ shared_prefix_kernel(const __grid_constant__ SharedParams p, const __grid_consta
     }
 }
 
-template <int D, int kTerms>
+// One warp per row of a flagged request: tail and prefix chunks joined by log-sum-exp, rounded once.  Chunks are
+// taken eight at a time, all their loads before the first use.
+template <int V, bool kBf16>
+__global__ void __launch_bounds__(256)
+shared_join_kernel(const __grid_constant__ SharedParams p)
+{
+    griddep_wait();
+    griddep_launch_dependents();
+    constexpr int D = V * 32, kBatch = 8;
+    const int lane = threadIdx.x & 31;
+    const long long rows = (long long)p.num_gated * p.batch * p.num_q_heads;
+    const SharedDesc& sd = *p.desc;
+    const int t1 = sd.t1, nseg = sd.nseg;
+    const long long total = sd.total;
+    for (long long w = ((long long)blockIdx.x * blockDim.x + threadIdx.x) >> 5; w < rows;
+         w += ((long long)gridDim.x * blockDim.x) >> 5) {
+        const int h = (int)(w % p.num_q_heads);
+        const int b = (int)((w / p.num_q_heads) % p.batch);
+        const int gl = (int)(w / ((long long)p.num_q_heads * p.batch));
+        if (!p.flags[b] || p.seq_lens[b] < 1) continue;
+        const int layer = p.layer[gl];
+        const SharedRow r = sd.rows[b];
+        const size_t tail = ((size_t)(layer - p.layer_begin) * p.batch + b) * p.num_q_heads + h;
+        float2 ml = p.tail_ml[tail];
+        float o[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) o[e] = p.tail_o[tail * D + lane * V + e];
+        if (r.tiles > 0) {
+            const int kvh = h / p.group;
+            const long long u0 = ((long long)gl * p.num_kv_heads + kvh) * t1 + r.unit;
+            const int j0 = (int)(((u0 + 1) * nseg - 1) / total);             // the spans of its first and last tile
+            const int j1 = (int)(((u0 + r.tiles) * nseg - 1) / total);
+            const size_t ext = p.ext_row0 + r.row + (h - kvh * p.group);
+            for (int c0 = j0; c0 <= j1; c0 += kBatch) {
+                float2 cm[kBatch];
+                float co[kBatch][V];
+#pragma unroll
+                for (int c = 0; c < kBatch; ++c) {
+                    const int j = c0 + c;
+                    if (j > j1) {
+                        cm[c] = make_float2(-INFINITY, 0.f);
+#pragma unroll
+                        for (int e = 0; e < V; ++e) co[c][e] = 0.f;
+                        continue;
+                    }
+                    const size_t row = j == j0 ? (size_t)w : ext + (size_t)j * 256;
+                    cm[c] = p.part_ml[row];
+#pragma unroll
+                    for (int e = 0; e < V; ++e) co[c][e] = p.part_o[row * D + lane * V + e];
+                }
+                float m = ml.x;
+#pragma unroll
+                for (int c = 0; c < kBatch; ++c) m = fmaxf(m, cm[c].x);
+                const float mu = m == -INFINITY ? 0.f : m;
+                const float a = ex2(ml.x - mu);
+                ml = make_float2(m, ml.y * a);
+#pragma unroll
+                for (int e = 0; e < V; ++e) o[e] *= a;
+#pragma unroll
+                for (int c = 0; c < kBatch; ++c) {
+                    const float f = ex2(cm[c].x - mu);
+                    ml.y += cm[c].y * f;
+#pragma unroll
+                    for (int e = 0; e < V; ++e) o[e] = fmaf(co[c][e], f, o[e]);
+                }
+            }
+        }
+        const float inv = 1.f / ml.y;
+        const size_t dst = ((size_t)layer * p.batch + b) * p.num_q_heads + h;
+#pragma unroll
+        for (int e = 0; e < V; e += 2) {
+            if constexpr (kBf16)
+                reinterpret_cast<__nv_bfloat162*>(p.out)[(dst * D + lane * V + e) / 2] = __floats2bfloat162_rn(o[e] * inv, o[e + 1] * inv);
+            else
+                reinterpret_cast<float2*>(p.out)[(dst * D + lane * V + e) / 2] = make_float2(o[e] * inv, o[e + 1] * inv);
+        }
+        if (p.lse && lane == 0) p.lse[dst] = (ml.x + log2f(ml.y)) * 0.6931471805599453f;
+    }
+}
+
+cudaError_t launch_shared_join(const SharedParams& p, int head_dim, bool out_bf16, cudaStream_t st, bool pdl)
+{
+    const long long rows = (long long)p.num_gated * p.batch * p.num_q_heads;
+    const dim3 grid((unsigned)std::min<long long>((rows + 7) / 8, 148 * 8));
+    if (head_dim == 128)
+        return out_bf16 ? launch_ex(shared_join_kernel<4, true>, grid, dim3(256), 0, st, pdl, p)
+                        : launch_ex(shared_join_kernel<4, false>, grid, dim3(256), 0, st, pdl, p);
+    return out_bf16 ? launch_ex(shared_join_kernel<2, true>, grid, dim3(256), 0, st, pdl, p)
+                    : launch_ex(shared_join_kernel<2, false>, grid, dim3(256), 0, st, pdl, p);
+}
+
+template <int D, int kTerms, bool kWide>
 static cudaError_t launch_shared_t(const SharedParams& p, const void* kmap, const void* vmap, int grid, cudaStream_t st, bool pdl)
 {
-    using C = ShCfg<D, kTerms>;
-    constexpr int smem = 2 * C::kQBytes + C::kSlots * C::kSlotBytes + (int)(sizeof(ShPlan) + 15) / 16 * 16 + (int)sizeof(ShCtl);
+    using C = ShCfg<D, kTerms, kWide>;
+    constexpr int smem = C::kQTiles * C::kQBytes + C::kSlots * C::kSlotBytes + (int)(sizeof(ShPlan) + 15) / 16 * 16 + (int)sizeof(ShCtl);
     static_assert(smem <= 232448, "shared memory");
-    cudaError_t e = cudaFuncSetAttribute(shared_prefix_kernel<D, kTerms>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    cudaError_t e = cudaFuncSetAttribute(shared_prefix_kernel<D, kTerms, kWide>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e != cudaSuccess) return e;
-    return launch_ex(shared_prefix_kernel<D, kTerms>, dim3(grid), dim3(kShThreads), smem, st, pdl, p,
+    return launch_ex(shared_prefix_kernel<D, kTerms, kWide>, dim3(grid), dim3(384), smem, st, pdl, p,
                      *reinterpret_cast<const CUtensorMap*>(kmap), *reinterpret_cast<const CUtensorMap*>(vmap));
 }
 
 cudaError_t launch_shared_prefix(const SharedParams& p, const void* kmap, const void* vmap, int head_dim, bool out_bf16,
                                  int grid, cudaStream_t st, bool pdl)
 {
-    if (head_dim == 128)
-        return out_bf16 ? launch_shared_t<128, 2>(p, kmap, vmap, grid, st, pdl) : launch_shared_t<128, 3>(p, kmap, vmap, grid, st, pdl);
-    return out_bf16 ? launch_shared_t<64, 2>(p, kmap, vmap, grid, st, pdl) : launch_shared_t<64, 3>(p, kmap, vmap, grid, st, pdl);
+    const bool wide = p.batch * p.group > kShRows;
+    if (head_dim == 128) {
+        if (wide)
+            return out_bf16 ? launch_shared_t<128, 2, true>(p, kmap, vmap, grid, st, pdl) : launch_shared_t<128, 3, true>(p, kmap, vmap, grid, st, pdl);
+        return out_bf16 ? launch_shared_t<128, 2, false>(p, kmap, vmap, grid, st, pdl) : launch_shared_t<128, 3, false>(p, kmap, vmap, grid, st, pdl);
+    }
+    if (wide)
+        return out_bf16 ? launch_shared_t<64, 2, true>(p, kmap, vmap, grid, st, pdl) : launch_shared_t<64, 3, true>(p, kmap, vmap, grid, st, pdl);
+    return out_bf16 ? launch_shared_t<64, 2, false>(p, kmap, vmap, grid, st, pdl) : launch_shared_t<64, 3, false>(p, kmap, vmap, grid, st, pdl);
 }
 
 }  // namespace oda

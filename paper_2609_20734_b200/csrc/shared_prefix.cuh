@@ -1,5 +1,5 @@
-// What the two kernels of the shared-prefix Full pass have in common: parameters of the first (shared_prefix.cu) and
-// the descriptor by which the second (splitkv_tma.cu, kInstFold) finds the partial results of a row.
+// What the three kernels of the shared-prefix Full pass have in common: the matrix kernel over the prefixes and the one
+// that joins (shared_prefix.cu), and between them the split-KV kernel over the tails (splitkv_tma.cu, kInstTail).
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -9,19 +9,77 @@
 
 namespace oda {
 
-struct SharedRow {   // one request
+struct __align__(16) SharedRow {   // one request
     int32_t unit;    // first tile of its row block within one (layer, kv head)
     int32_t tiles;   // tiles of its prefix (0: it shares nothing)
     int32_t row;     // its first row within the row block
+    int32_t pad;
 };
 
 // Partial results of a row over its prefix: chunk 0 at row ((gated layer) * batch + b) * q_heads + head, chunk c > 0 at
 // ext_row0 + (first span + c) * 256 + row + head within the group.
 struct SharedDesc {
-    int32_t t1, total, nseg;         // tiles of one (layer, kv head), of all, spans they are cut into
+    int32_t t1, total, nseg, pad;    // tiles of one (layer, kv head), of all, spans they are cut into
     int32_t gated_index[kMaxLayers]; // layer -> its place among the call's gated layers
     SharedRow rows[kMaxBatch];
 };
+
+// Who shares what.  The first two kernels work it out by themselves, from the device-resident lengths, flags and groups.
+struct SharedGroups {                // shared memory
+    int32_t t[kMaxBatch];            // lengths, clamped to the table
+    int32_t gs[kMaxBatch + 1];
+    int32_t pages[kMaxBatch];        // shared pages of the group (0: shares nothing)
+    uint8_t members[kMaxBatch];      // flagged requests of the group
+    uint8_t act[kMaxBatch];
+    uint8_t list[kMaxBatch];         // flagged requests, those of group i from gs[i] on
+};
+
+// Called by all threads of a CTA (at least 129); ends with a barrier.  `report`: this CTA sets the status bits.
+__device__ __forceinline__ void shared_groups(SharedGroups& g, int batch, int max_blocks, const int32_t* seq_lens,
+                                              const uint8_t* flags, int num_groups, const int32_t* group_start,
+                                              const int32_t* group_prefix, int32_t* status, bool report)
+{
+    const int tid = threadIdx.x;
+    const long long cap = (long long)max_blocks * kPage;
+    if (tid < batch) {
+        const int t = seq_lens[tid], f = flags[tid];
+        g.t[tid] = (int)min((long long)t, cap);
+        g.act[tid] = f && t >= 1;
+        if (report && f && t > cap) atomicOr(status, kStatusBadSeqLen);
+    }
+    const int prefix = tid < num_groups ? group_prefix[tid] : 0;
+    if (num_groups > 0 && tid <= num_groups) g.gs[tid] = group_start[tid];
+    __syncthreads();
+    if (tid < num_groups) {
+        const int s = g.gs[tid], e = g.gs[tid + 1];
+        bool ok = s >= 0 && e >= s && e <= batch;
+        for (int k = 0; k < tid; ++k) ok = ok && g.gs[k] <= s;  // nobody belongs to two groups
+        int n = 0, least = 0x7fffffff;
+        if (ok) {
+            for (int b = s; b < e; ++b)
+                if (g.act[b]) {
+                    g.list[s + n++] = (uint8_t)b;
+                    least = min(least, g.t[b]);
+                }
+        } else if (report) {
+            atomicOr(status, kStatusBadGroup);
+        }
+        // a lone request shares with nobody; everybody keeps a position of his own
+        const int shared = n >= 2 ? min(prefix, least - 1) : 0;
+        g.pages[tid] = shared > 0 ? shared / kPage : 0;
+        g.members[tid] = (uint8_t)n;
+    }
+    __syncthreads();
+}
+
+// the group that request b shares with (-1: none)
+__device__ __forceinline__ int shared_group_of(const SharedGroups& g, int num_groups, int b)
+{
+    if (!g.act[b]) return -1;
+    for (int i = 0; i < num_groups; ++i)
+        if (g.pages[i] > 0 && b >= g.gs[i] && b < g.gs[i + 1]) return i;
+    return -1;
+}
 
 struct SharedParams {
     const __nv_bfloat16* q;
@@ -32,12 +90,14 @@ struct SharedParams {
     const int32_t* group_prefix;
     int32_t* status;
     SharedDesc* desc;
-    int32_t* page_shift;             // [batch] pages that the second kernel skips
-    int32_t* tail_lens;              // [batch] positions that it sees
     float* part_o;                   // [rows][D] unnormalised
     float2* part_ml;                 // [rows] (m in log2 units, l)
+    float* tail_o;                   // the same of the tails, [layers of the call][batch][q heads]
+    float2* tail_ml;
+    void* out;
+    float* lse;                      // nullable
     size_t ext_row0;
-    int32_t batch, num_groups, num_q_heads, num_kv_heads, group, max_blocks_per_seq, num_gated, blocks_per_layer;
+    int32_t batch, num_groups, num_q_heads, num_kv_heads, group, max_blocks_per_seq, num_gated, blocks_per_layer, layer_begin;
     float scale_log2e;
     uint8_t layer[kMaxLayers];       // the call's gated layers
     uint16_t kv_index[kMaxLayers];   // and their cache slices
@@ -45,5 +105,6 @@ struct SharedParams {
 
 cudaError_t launch_shared_prefix(const SharedParams& p, const void* kmap, const void* vmap, int head_dim, bool out_bf16,
                                  int grid, cudaStream_t st, bool pdl);
+cudaError_t launch_shared_join(const SharedParams& p, int head_dim, bool out_bf16, cudaStream_t st, bool pdl);
 
 }  // namespace oda

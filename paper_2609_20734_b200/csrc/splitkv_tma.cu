@@ -59,7 +59,9 @@ struct TmaCfg {
     static constexpr int kQSlotBytes = 8 * D * 2;           // q of one kv-head group (up to 8 heads)
     static constexpr int kMergeBytes = 32 * 32 * 4 + 32 * 4 * 4;  // one warp's O fragment + (m, l) of two heads per lane
     static constexpr int kSmemBytes = kStages * (kStageBytes + kQSlotBytes) + kMergeBytes + (int)sizeof(Plan) + (int)sizeof(Ctl);
+    static constexpr int kTailBytes = kMaxBatch * 4;  // kInstTail: pages that each request skips
     static_assert(kStages <= kMaxStages, "ring deeper than the control block");
+    static_assert(2 * (kSmemBytes + kTailBytes + 1024) <= 233472, "two CTAs per SM");
 };
 
 // ------------------------------------------------------------------ PTX helpers (mbarriers: mbar.cuh)
@@ -159,10 +161,12 @@ struct PageRun {
 //                weights up.  It keeps P as three bf16 parts: 24 bits, so that fp32 results are as good
 //                as fp32 arithmetic makes them (two parts leave 1.6e-6 of the result; the third product
 //                is hidden behind the stream).
-//  kInstFold     the tails of requests that share prefixes: it skips the shared pages and folds the partial
-//                results over the prefix (shared_prefix.cu) into each row before it is stored.  Three parts
-//                of P like kInstScores.
-constexpr int kInstGeneral = 0, kInstUniform = 1, kInstScores = 2, kInstFold = 3;
+//  kInstTail     the tails of requests that share prefixes (shared_prefix.cu): it skips the shared pages and
+//                leaves each row as a partial result.  Three parts of P like kInstScores.  It runs beside the
+//                kernel before it: that one lets its dependents start only once everything before IT has
+//                finished, so lengths, flags and caches are final, and nothing here reads what it writes.  Every
+//                CTA waits for it before it ends, so that what follows this kernel follows both.
+constexpr int kInstGeneral = 0, kInstUniform = 1, kInstScores = 2, kInstTail = 3;
 template <int D, int G, int kInst>
 __global__ void __launch_bounds__(TmaCfg<D>::kThreads, 2)
 splitkv_tma_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtensorMap kmap,
@@ -177,6 +181,7 @@ splitkv_tma_kernel(const __grid_constant__ AttnParams p, const __grid_constant__
     float* mlbuf = mbuf + 32 * 32;                                        // [32][4]
     Plan& plan = *reinterpret_cast<Plan*>(mlbuf + 32 * 4);
     Ctl& ctl = *reinterpret_cast<Ctl*>(reinterpret_cast<uint8_t*>(&plan) + sizeof(Plan));
+    int32_t* page_shift = reinterpret_cast<int32_t*>(reinterpret_cast<uint8_t*>(&ctl) + sizeof(Ctl));  // kInstTail: [kMaxBatch]
     const uint32_t full0 = smem_u32(ctl.full), empty0 = smem_u32(ctl.empty);
     const uint32_t efull = smem_u32(&ctl.efull), efree = smem_u32(&ctl.efree);
 
@@ -216,7 +221,7 @@ splitkv_tma_kernel(const __grid_constant__ AttnParams p, const __grid_constant__
         dp.t = ld_meta_s32(p.seq_lens);
     }
     __syncthreads();      // the barriers are initialised for every warp
-    if (!early_try) griddep_wait();  // everything above is independent of the previous kernel in the stream
+    if (kInst != kInstTail && !early_try) griddep_wait();  // everything above is independent of the previous kernel in the stream
     // same registers in every thread: no barrier, no shared plan
     if (direct_try && direct_rule(p, dp.t)) dp.ok = 1;
     if constexpr (kUniform) {
@@ -230,15 +235,35 @@ splitkv_tma_kernel(const __grid_constant__ AttnParams p, const __grid_constant__
     } else {
         if (gated_pass_is_empty(p)) {
             griddep_launch_dependents();
+            if constexpr (kInst == kInstTail) griddep_wait();
             return;
         }
-        build_plan(p, plan);  // ends with a barrier
+        if constexpr (kInst == kInstTail) {
+            // working memory of the plan: the hand-off buffer of the epilogue warp, not in use yet
+            static_assert(sizeof(SharedGroups) + kMaxBatch * 4 <= 32 * 32 * 4, "hand-off buffer");
+            SharedGroups& sg = *reinterpret_cast<SharedGroups*>(mbuf);
+            int32_t* tails = reinterpret_cast<int32_t*>(mbuf) + 1024 - kMaxBatch;
+            shared_groups(sg, p.batch, p.max_blocks_per_seq, p.seq_lens, p.flags, p.num_groups, p.group_start, p.group_prefix,
+                          p.status, false);
+            if (tid < p.batch) {
+                const int i = shared_group_of(sg, p.num_groups, tid);
+                page_shift[tid] = i < 0 ? 0 : sg.pages[i];
+                tails[tid] = sg.t[tid] - page_shift[tid] * kPage;
+            }
+            __syncthreads();
+            build_plan(p, plan, tails);
+        } else {
+            build_plan(p, plan);  // ends with a barrier
+        }
         span = plan.my_span;
     }
     griddep_launch_dependents();
     volatile int* abort_flag = &ctl.abort;
     constexpr uint32_t kQBytes = G * D * 2;
-    if (span < 0) return;
+    if (span < 0) {
+        if constexpr (kInst == kInstTail) griddep_wait();
+        return;
+    }
 
     if (warp == C::kProducerWarp) {
         // ============================ producer warp ============================
@@ -269,7 +294,7 @@ splitkv_tma_kernel(const __grid_constant__ AttnParams p, const __grid_constant__
             if (item_first) { r.item = it; r.take = take; }
             item_first = false;
             const int32_t* table = p.block_table + (size_t)it.b * p.max_blocks_per_seq;
-            if constexpr (kInst == kInstFold) table += __ldcg(p.page_shift + it.b);
+            if constexpr (kInst == kInstTail) table += page_shift[it.b];
             blk = lane < r.n ? __ldg(table + item_logical_page(it, v + lane)) : 0;
             v += r.n;
             if (v >= nv) {
@@ -350,44 +375,21 @@ splitkv_tma_kernel(const __grid_constant__ AttnParams p, const __grid_constant__
         // 128-bit loads and stores the result straight from the fragment.
         const int hrow = lane >> 2, qc = (lane & 3) * 2;
         const float kLn2 = 0.6931471805599453f;
-        // folds the partial results over the request's shared prefix into the row, chunk after chunk
-        auto fold_shared = [&](const Item& it, float (&o)[D / 16][4], float4& ml) {
-            const SharedDesc& sd = *p.shared;
-            const int tiles = __ldcg(&sd.rows[it.b].tiles);
-            if (tiles == 0) return;
-            const int gl = __ldcg(&sd.gated_index[it.layer]), nseg = __ldcg(&sd.nseg);
-            const long long total = __ldcg(&sd.total);
-            const long long u0 = ((long long)gl * p.num_kv_heads + it.g) * __ldcg(&sd.t1) + __ldcg(&sd.rows[it.b].unit);
-            const int j0 = (int)(((u0 + 1) * nseg - 1) / total);            // the spans of its first and last tile
-            const int j1 = (int)(((u0 + tiles) * nseg - 1) / total);
-            const size_t own = ((size_t)gl * p.batch + it.b) * p.num_q_heads + it.g * G;
-            const size_t ext = p.shared_ext_row0 + __ldcg(&sd.rows[it.b].row);
-            for (int j = j0; j <= j1; ++j) {
-                const size_t row = j == j0 ? own : ext + (size_t)j * 256;
+        auto store_final = [&](const Item& it, const float (&o)[D / 16][4], const float4& ml) {
+            if constexpr (kInst == kInstTail) {  // the row as a partial, for the kernel that joins it with its prefix
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     if (qc + e >= G) continue;
-                    const float2 pm = __ldcg(p.shared_ml + row + qc + e);
-                    const float* src = p.shared_o + (row + qc + e) * D + hrow;
-                    float v[D / 8];
-#pragma unroll
-                    for (int n = 0; n < D / 8; ++n) v[n] = __ldcg(src + n * 8);
-                    float& mm = e ? ml.z : ml.x;
-                    float& ll = e ? ml.w : ml.y;
-                    const float mn = fmaxf(mm, pm.x), mu = mn == -INFINITY ? 0.f : mn;
-                    const float a = ex2(mm - mu), c = ex2(pm.x - mu);
-                    mm = mn;
-                    ll = ll * a + pm.y * c;
+                    const size_t row = ((size_t)(it.layer - p.layer_begin) * p.batch + it.b) * p.num_q_heads + it.g * G + qc + e;
 #pragma unroll
                     for (int n = 0; n < D / 16; ++n) {
-                        o[n][e] = o[n][e] * a + v[2 * n] * c;
-                        o[n][2 + e] = o[n][2 + e] * a + v[2 * n + 1] * c;
+                        __stcg(p.tail_o + row * D + hrow + n * 16, o[n][e]);
+                        __stcg(p.tail_o + row * D + hrow + n * 16 + 8, o[n][2 + e]);
                     }
+                    if (hrow == 0) __stcg(p.tail_ml + row, e ? make_float2(ml.z, ml.w) : make_float2(ml.x, ml.y));
                 }
+                return;
             }
-        };
-        auto store_final = [&](const Item& it, float (&o)[D / 16][4], float4 ml) {
-            if constexpr (kInst == kInstFold) fold_shared(it, o, ml);
             // remainder mode: the Local lse is read by every lane of a head before any lane replaces it
             float l_old2[2] = {0.f, 0.f};
             if (p.mode == 2) {
@@ -552,6 +554,7 @@ splitkv_tma_kernel(const __grid_constant__ AttnParams p, const __grid_constant__
                 }
             }
         }
+        if constexpr (kInst == kInstTail) griddep_wait();
         return;
     }
 
@@ -880,7 +883,7 @@ template <int D, int G, int kInst>
 static cudaError_t prepare_tma_t()
 {
     cudaError_t e = cudaFuncSetAttribute(splitkv_tma_kernel<D, G, kInst>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                         TmaCfg<D>::kSmemBytes);
+                                         TmaCfg<D>::kSmemBytes + (kInst == kInstTail ? TmaCfg<D>::kTailBytes : 0));
     if (e != cudaSuccess) return e;
     (void)cudaFuncSetAttribute(splitkv_tma_kernel<D, G, kInst>, cudaFuncAttributePreferredSharedMemoryCarveout,
                                cudaSharedmemCarveoutMaxShared);
@@ -896,7 +899,7 @@ static cudaError_t launch_tma_t(const AttnParams& p, const void* kmap, const voi
         cudaError_t e = prepare_tma_t<D, G, kInstGeneral>();
         if (e == cudaSuccess) e = prepare_tma_t<D, G, kInstUniform>();
         if (e == cudaSuccess) e = prepare_tma_t<D, G, kInstScores>();
-        if (e == cudaSuccess) e = prepare_tma_t<D, G, kInstFold>();
+        if (e == cudaSuccess) e = prepare_tma_t<D, G, kInstTail>();
         if (e != cudaSuccess) return e;
         attr_set = true;
     }
@@ -905,8 +908,8 @@ static cudaError_t launch_tma_t(const AttnParams& p, const void* kmap, const voi
     const dim3 g(grid), t(TmaCfg<D>::kThreads);
     if (p.score_rows)
         return launch_ex(splitkv_tma_kernel<D, G, kInstScores>, g, t, TmaCfg<D>::kSmemBytes, st, pdl, p, km, vm, blocks_per_layer);
-    if (p.shared)
-        return launch_ex(splitkv_tma_kernel<D, G, kInstFold>, g, t, TmaCfg<D>::kSmemBytes, st, pdl, p, km, vm, blocks_per_layer);
+    if (p.tail_o)
+        return launch_ex(splitkv_tma_kernel<D, G, kInstTail>, g, t, TmaCfg<D>::kSmemBytes + TmaCfg<D>::kTailBytes, st, pdl, p, km, vm, blocks_per_layer);
     if (p.uniform_hint && !p.direct_hint)
         return launch_ex(splitkv_tma_kernel<D, G, kInstUniform>, g, t, TmaCfg<D>::kSmemBytes, st, pdl, p, km, vm, blocks_per_layer);
     return launch_ex(splitkv_tma_kernel<D, G, kInstGeneral>, g, t, TmaCfg<D>::kSmemBytes, st, pdl, p, km, vm, blocks_per_layer);
