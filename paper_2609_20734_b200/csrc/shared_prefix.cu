@@ -16,7 +16,7 @@
 // (layer, kv head, group, row block, tile) lie on one axis that is cut into equal spans, one per CTA (one CTA per SM).
 // A unit that a span boundary cuts leaves several partials; nobody waits for another CTA.
 //
-// A CTA: two softmax warpgroups ("streams"), an MMA warp for each (one thread issues) and a producer warp (TMA).  With more than
+// A CTA: two softmax warpgroups ("streams"), an MMA warp for each (one thread issues) and two producer warps (TMA).  With more than
 // 128 rows the streams are the two row tiles and both use every K/V tile; with fewer, both have the same rows and take
 // the tiles in turn (stream 0 the even ones), and their results are joined through TMEM at the end.  Either way one
 // stream's softmax runs while the tensor core works for the other.  TMEM: S of both streams (kTokens columns each; P
@@ -295,7 +295,7 @@ shared_prefix_kernel(const __grid_constant__ SharedParams p, const __grid_consta
     volatile int* abort_flag = &ctl.abort;
     if (tid == 0) {
         for (int s = 0; s < C::kSlots; ++s) {
-            mbar_init(smem_u32(&ctl.full[s]), 1);
+            mbar_init(smem_u32(&ctl.full[s]), 2);
             mbar_init(smem_u32(&ctl.empty[s]), kWide ? 2 : 1);
         }
         for (int s = 0; s < 2; ++s) {
@@ -330,8 +330,11 @@ shared_prefix_kernel(const __grid_constant__ SharedParams p, const __grid_consta
     // 256 x 216 + 128 x 72)
     if (warp >= 8) {
     if constexpr (kWide) asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
-    if (warp == 8) {
-        // ============================ producer warp ============================
+    if (warp == 8 || warp == 11) {
+        // ============================ producer warps ============================
+        // Each issues half of every tensor's boxes: a warp spends about 125 cycles on a box, and the 12 boxes of
+        // a 64-position tile (1,400 cycles of DRAM's time) were more than one warp could issue.
+        const int half = warp == 8 ? 0 : 1;
         const uint64_t once = 0x12F0000000000000ull;    // L2 evict-first: read by one row block
         const uint64_t again = 0x1000000000000000ull;   // L2 evict-normal: the next row block reads it too
         uint32_t cnt = 0;
@@ -363,16 +366,23 @@ shared_prefix_kernel(const __grid_constant__ SharedParams p, const __grid_consta
                 const uint32_t s = cnt % C::kSlots, ph = (cnt / C::kSlots) & 1;
                 if (!warp_wait(&ctl.empty[s], ph ^ 1, abort_flag, p.status)) return false;
                 const uint32_t bar = smem_u32(&ctl.full[s]);
-                if (lane == 0) mbar_expect_tx(bar, (uint32_t)np * kPage * D * 2);
-                __syncwarp();
                 const uint32_t dst = smem_u32(ring + s * C::kSlotBytes);
                 if (is_v) {  // one box: the page of the head, slab after slab
-                    const int blk = __shfl_sync(0xffffffffu, ids, (pg - base + (lane & (TP - 1))) & 31);
-                    if (lane < np) tma_box(dst + lane * (kPage * D * 2), &vmap, bar, 0, it.kvh, kv0 + blk, policy);
-                } else {     // one box per slab: a slab's rows of all pages lie one behind the other
-                    const int pgi = lane % TP, slab = lane / TP;
+                    const int pgi = half * (TP / 2) + lane;
+                    const bool mine = lane < TP / 2 && pgi < np;
                     const int blk = __shfl_sync(0xffffffffu, ids, (pg - base + pgi) & 31);
-                    if (pgi < np && slab < kSlabs) tma_box(dst + slab * (TN * 128) + pgi * 2048, &kmap, bar, slab, it.kvh, kv0 + blk, policy);
+                    if (lane == 0) mbar_expect_tx(bar, (uint32_t)max(0, min(TP / 2, np - half * (TP / 2))) * (kPage * D * 2));
+                    __syncwarp();
+                    if (mine) tma_box(dst + pgi * (kPage * D * 2), &vmap, bar, 0, it.kvh, kv0 + blk, policy);
+                } else {     // one box per slab: a slab's rows of all pages lie one behind the other
+                    constexpr int kEach = kSlabs * TP / 2;
+                    const int e = half * kEach + lane, pgi = e % TP, slab = e / TP;
+                    const bool mine = lane < kEach && pgi < np;
+                    const int blk = __shfl_sync(0xffffffffu, ids, (pg - base + pgi) & 31);
+                    const uint32_t boxes = __popc(__ballot_sync(0xffffffffu, mine));
+                    if (lane == 0) mbar_expect_tx(bar, boxes * (kPage * 128));
+                    __syncwarp();
+                    if (mine) tma_box(dst + slab * (TN * 128) + pgi * 2048, &kmap, bar, slab, it.kvh, kv0 + blk, policy);
                 }
                 ++cnt;
                 return true;
@@ -390,7 +400,7 @@ shared_prefix_kernel(const __grid_constant__ SharedParams p, const __grid_consta
             const uint32_t c2 = cnt - 1 - k;
             if (!warp_wait(&ctl.empty[c2 % C::kSlots], (c2 / C::kSlots) & 1, abort_flag, p.status)) break;
         }
-    } else if (warp < 11) {
+    } else {
         // ============================ MMA warps: one per stream, one thread issues ============================
         // (The loop is run by the whole warp on warp-uniform values, and descriptors differ by constants: a thread
         // that computes them anew before each product issues one in 100 cycles, slower than they run.  One warp for
