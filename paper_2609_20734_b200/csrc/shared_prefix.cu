@@ -16,16 +16,17 @@
 // (layer, kv head, group, row block, tile) lie on one axis that is cut into equal spans, one per CTA (one CTA per SM).
 // A unit that a span boundary cuts leaves several partials; nobody waits for another CTA.
 //
-// A CTA: two softmax warpgroups ("streams"), an MMA warp for each (one thread issues) and two producer warps (TMA).  With more than
-// 128 rows the streams are the two row tiles and both use every K/V tile; with fewer, both have the same rows and take
-// the tiles in turn (stream 0 the even ones), and their results are joined through TMEM at the end.  Either way one
-// stream's softmax runs while the tensor core works for the other.  TMEM: S of both streams (kTokens columns each; P
-// replaces S in place as bf16) and O of both streams (D columns each).
+// A CTA: two softmax warpgroups ("streams"), an MMA warp for each (one thread issues) and two producer warps (TMA).  With
+// more than 128 rows the streams are the two row tiles and both use every K/V tile; with fewer, both have the same rows
+// and take the tiles in turn (stream 0 the even ones), and their results are joined through TMEM at the end.  TMEM: S
+// (then P in its place, as bf16) in kBufs buffers a stream, and O of both streams.
 //
 // Two forms of the kernel, chosen by the most rows that a kv head can have in the call (batch x group):
-//   narrow (<= 128 rows): bound by the stream of K and V.  Tiles of 64 positions, one copy of Q, and the rest of shared
-//     memory as a ring: what waits for its softmax is small, what is on its way large.
-//   wide: bound by the products and the exponentials.  Tiles of 128 positions and 2 x 128 rows.
+//   narrow (<= 128 rows): bound by the stream of K and V.  One copy of Q, and the rest of shared memory as a ring.
+//   wide: bound by the products and the exponentials.  2 x 128 rows, and S twice for each: while the softmax of a tile
+//     runs, the product for the next one has been made, so that neither waits for the other.  (With S once, the two
+//     streams fall into step -- both compute exponentials, then both wait for products -- and a pair of
+//     128-position tiles took 6,000 cycles.)
 //
 // P in bf16 is kTerms parts of 8 bits each.  fp32 results take three (24 bits: nothing is lost against fp32
 // arithmetic), bf16 results two in the narrow form, where the second product hides behind the stream.
@@ -46,17 +47,20 @@ constexpr int kShMinTiles = 2;     // a CTA is not given fewer tiles than this (
 
 template <int D, int kTerms, bool kWide>
 struct ShCfg {
-    static constexpr int kTokens = kWide && kTerms < 3 ? 128 : 64;
+    static constexpr int kTokens = 64;
     static constexpr int kTilePages = kTokens / kPage;
-    static constexpr int kSlotBytes = kTokens * D * 2;      // K or V of one tile
+    static constexpr int kTileBytes = kTokens * D * 2;      // K or V of one tile
+    static constexpr int kSlotBytes = 2 * kTileBytes;       // V of a tile, and behind it the K that is needed next
     static constexpr int kRing = kWide ? 131072 : 180224;
-    static constexpr int kSlots = kRing / kSlotBytes > 16 ? 16 : kRing / kSlotBytes;
+    static constexpr int kSlots = kRing / kSlotBytes;
     static constexpr int kQBytes = kShRows * D * 2;
     static constexpr int kQTiles = kWide ? 2 : 1;
-    static constexpr int kSpCols = kTokens / 2 * kTerms > kTokens ? kTokens / 2 * kTerms : kTokens;  // one stream's S, then P
-    static constexpr int kO0 = 2 * kSpCols;                 // first column of stream 0's O
+    static constexpr int kSpCols = kTokens / 2 * kTerms > kTokens ? kTokens / 2 * kTerms : kTokens;  // one S, then P
+    static constexpr int kBufs = kWide && 4 * kSpCols + 2 * D <= 512 ? 2 : 1;
+    static constexpr int kO0 = 2 * kBufs * kSpCols;         // first column of stream 0's O
     static constexpr int kRowBlock = kWide ? 256 : 128;     // rows of a unit
-    static_assert(2 * kSpCols + 2 * D <= 512, "TMEM");
+    static_assert(kO0 + 2 * D <= 512, "TMEM");
+    static_assert(kSlots <= 12, "control block");
 };
 
 struct ShPlan {
@@ -66,8 +70,9 @@ struct ShPlan {
 };
 
 struct ShCtl {
-    uint64_t full[16], empty[16];
-    uint64_t s_full[2], p_full[2], o_full[2], q_full[2];
+    uint64_t full[12], empty[12];
+    uint64_t s_full[2][2], p_full[2][2], pv_done[2][2];  // [stream][buffer]
+    uint64_t q_full[2];
     uint64_t ml_full, o1_read;       // joining the streams: stream 1's (m, l) are there, its O has been read
     uint32_t tmem;
     int32_t abort;
@@ -191,10 +196,15 @@ __device__ __forceinline__ void tma_box(uint32_t dst, const CUtensorMap* map, ui
         ::"r"(dst), "l"(map), "r"(0), "r"(0), "r"(slab), "r"(head), "r"(block), "r"(bar), "l"(policy)
         : "memory");
 }
-// bounded wait with one answer for the whole warp
+// Bounded wait with one answer for the whole warp.  The first tries do without the clock: reading the global timer costs
+// some hundred cycles, which a wait for another warp of the CTA would notice every time.
 __device__ __forceinline__ bool warp_wait(const uint64_t* bar, uint32_t parity, volatile int* abort_flag, int* status)
 {
-    return __all_sync(0xffffffffu, mbar_wait(smem_u32(bar), parity, abort_flag, status));
+    const uint32_t a = smem_u32(bar);
+    bool ok = false;
+    for (int i = 0; i < 64 && !ok; ++i) ok = mbar_try_wait(a, parity);
+    if (!ok) ok = mbar_wait(a, parity, abort_flag, status);
+    return __all_sync(0xffffffffu, ok);
 }
 
 // ------------------------------------------------------------------ plan
@@ -299,9 +309,11 @@ shared_prefix_kernel(const __grid_constant__ SharedParams p, const __grid_consta
             mbar_init(smem_u32(&ctl.empty[s]), kWide ? 2 : 1);
         }
         for (int s = 0; s < 2; ++s) {
-            mbar_init(smem_u32(&ctl.s_full[s]), 1);
-            mbar_init(smem_u32(&ctl.p_full[s]), 4);
-            mbar_init(smem_u32(&ctl.o_full[s]), 1);
+            for (int u = 0; u < 2; ++u) {
+                mbar_init(smem_u32(&ctl.s_full[s][u]), 1);
+                mbar_init(smem_u32(&ctl.p_full[s][u]), 4);
+                mbar_init(smem_u32(&ctl.pv_done[s][u]), 1);
+            }
             mbar_init(smem_u32(&ctl.q_full[s]), 4);
         }
         mbar_init(smem_u32(&ctl.ml_full), 4);
@@ -332,7 +344,7 @@ shared_prefix_kernel(const __grid_constant__ SharedParams p, const __grid_consta
     if constexpr (kWide) asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
     if (warp == 8 || warp == 11) {
         // ============================ producer warps ============================
-        // Each issues half of every tensor's boxes: a warp spends about 125 cycles on a box, and the 12 boxes of
+        // Each issues half of every slot's boxes: a warp spends about 125 cycles on a box, and the 12 boxes of
         // a 64-position tile (1,400 cycles of DRAM's time) were more than one warp could issue.
         const int half = warp == 8 ? 0 : 1;
         const uint64_t once = 0x12F0000000000000ull;    // L2 evict-first: read by one row block
@@ -342,7 +354,7 @@ shared_prefix_kernel(const __grid_constant__ SharedParams p, const __grid_consta
         for (int x = x0; x < x1 && !dead;) {
             const ShItem it = shared_item<TP, C::kRowBlock>(p, pl, x, x1);
             x += it.n;
-            const int ahead = kWide && it.nrows > kShRows ? 1 : 2;
+            const int ahead = kWide && it.nrows > kShRows ? C::kBufs : 2;
             const int lead = pl.g.list[pl.g.gs[it.group]];
             const int32_t* table = p.block_table + (size_t)lead * p.max_blocks_per_seq;
             const int first = it.tile0 * TP, last = min(it.pages, (it.tile0 + it.n) * TP);
@@ -354,45 +366,44 @@ shared_prefix_kernel(const __grid_constant__ SharedParams p, const __grid_consta
             ids_k.base = ids_v.base = first;
             ids_k.now = ids_v.now = fetch(first);
             ids_k.next = ids_v.next = fetch(first + 32);
-            auto load = [&](int tile, bool is_v) {
-                const int pg = first + tile * TP, np = min(TP, last - pg);
-                Ids& id = is_v ? ids_v : ids_k;
+            auto block_of = [&](Ids& id, int pg, int pgi) {
                 if (pg - id.base >= 32) {
                     id.base += 32;
                     id.now = id.next;
                     id.next = fetch(id.base + 32);
                 }
-                const int base = id.base, ids = id.now;
+                return kv0 + __shfl_sync(0xffffffffu, id.now, (pg - id.base + pgi) & 31);
+            };
+            // one slot: V of tile tv and K of tile tk (-1: none)
+            auto load = [&](int tv, int tk) {
                 const uint32_t s = cnt % C::kSlots, ph = (cnt / C::kSlots) & 1;
                 if (!warp_wait(&ctl.empty[s], ph ^ 1, abort_flag, p.status)) return false;
-                const uint32_t bar = smem_u32(&ctl.full[s]);
-                const uint32_t dst = smem_u32(ring + s * C::kSlotBytes);
-                if (is_v) {  // one box: the page of the head, slab after slab
-                    const int pgi = half * (TP / 2) + lane;
-                    const bool mine = lane < TP / 2 && pgi < np;
-                    const int blk = __shfl_sync(0xffffffffu, ids, (pg - base + pgi) & 31);
-                    if (lane == 0) mbar_expect_tx(bar, (uint32_t)max(0, min(TP / 2, np - half * (TP / 2))) * (kPage * D * 2));
-                    __syncwarp();
-                    if (mine) tma_box(dst + pgi * (kPage * D * 2), &vmap, bar, 0, it.kvh, kv0 + blk, policy);
-                } else {     // one box per slab: a slab's rows of all pages lie one behind the other
-                    constexpr int kEach = kSlabs * TP / 2;
-                    const int e = half * kEach + lane, pgi = e % TP, slab = e / TP;
-                    const bool mine = lane < kEach && pgi < np;
-                    const int blk = __shfl_sync(0xffffffffu, ids, (pg - base + pgi) & 31);
-                    const uint32_t boxes = __popc(__ballot_sync(0xffffffffu, mine));
-                    if (lane == 0) mbar_expect_tx(bar, boxes * (kPage * 128));
-                    __syncwarp();
-                    if (mine) tma_box(dst + slab * (TN * 128) + pgi * 2048, &kmap, bar, slab, it.kvh, kv0 + blk, policy);
+                const uint32_t bar = smem_u32(&ctl.full[s]), dst = smem_u32(ring + s * C::kSlotBytes);
+                constexpr int kEach = kSlabs * TP / 2;
+                const int vi = half * (TP / 2) + lane, ke = half * kEach + lane, ki = ke % TP, slab = ke / TP;
+                bool mv = false, mk = false;
+                int bv = 0, bk = 0;
+                if (tv >= 0) {  // one box: the page of the head, slab after slab
+                    const int pg = first + tv * TP;
+                    mv = lane < TP / 2 && pg + vi < last;
+                    bv = block_of(ids_v, pg, vi);
                 }
+                if (tk >= 0) {  // one box per slab: a slab's rows of all pages lie one behind the other
+                    const int pg = first + tk * TP;
+                    mk = lane < kEach && pg + ki < last;
+                    bk = block_of(ids_k, pg, ki);
+                }
+                const uint32_t bytes = __popc(__ballot_sync(0xffffffffu, mv)) * (kPage * D * 2) + __popc(__ballot_sync(0xffffffffu, mk)) * (kPage * 128);
+                if (lane == 0) mbar_expect_tx(bar, bytes);
+                __syncwarp();
+                if (mv) tma_box(dst + vi * (kPage * D * 2), &vmap, bar, 0, it.kvh, bv, policy);
+                if (mk) tma_box(dst + C::kTileBytes + slab * (TN * 128) + ki * 2048, &kmap, bar, slab, it.kvh, bk, policy);
                 ++cnt;
                 return true;
             };
             bool ok = true;
-            for (int t = 0; t < min(ahead, it.n) && ok; ++t) ok = load(t, false);
-            for (int t = 0; t < it.n && ok; ++t) {
-                ok = load(t, true);
-                if (ok && t + ahead < it.n) ok = load(t + ahead, false);
-            }
+            for (int t = 0; t < min(ahead, it.n) && ok; ++t) ok = load(-1, t);
+            for (int t = 0; t < it.n && ok; ++t) ok = load(t, t + ahead < it.n ? t + ahead : -1);
             dead = !ok;
         }
         // do not leave while copies may still be landing: every armed slot has been released (bounded)
@@ -409,11 +420,11 @@ shared_prefix_kernel(const __grid_constant__ SharedParams p, const __grid_consta
         constexpr uint32_t idesc_s = idesc_bf16(TN, false), idesc_o = idesc_bf16(D, true);
         const bool leader = elect_one();
         const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
-        const uint32_t ts = tm + s * C::kSpCols, to = tm + C::kO0 + s * D;  // S, then P; O
+        const uint32_t sp0 = tm + s * C::kBufs * C::kSpCols, to = tm + C::kO0 + s * D;  // S, then P; O
         const uint32_t q_lo = smem_lo(smem_u32(qs), 16) + (kWide ? s : 0) * (C::kQBytes >> 4);
-        const uint32_t k_lo = smem_lo(smem_u32(ring), 16), v_lo = smem_lo(smem_u32(ring), 2048);
-        uint32_t base = 0;               // tensors in the ring before the item
-        uint32_t nq = 0, np = 0;
+        const uint32_t k_lo = smem_lo(smem_u32(ring) + C::kTileBytes, 16), v_lo = smem_lo(smem_u32(ring), 2048);
+        uint32_t base = 0;               // slots before the item
+        uint32_t nq = 0, np[2] = {0, 0};
         bool ok = true;
         for (int x = x0; x < x1 && ok;) {
             const ShItem item = shared_item<TP, C::kRowBlock>(p, pl, x, x1);
@@ -421,82 +432,79 @@ shared_prefix_kernel(const __grid_constant__ SharedParams p, const __grid_consta
             const int n = __shfl_sync(0xffffffffu, item.n, 0);
             const bool dual = kWide && __shfl_sync(0xffffffffu, item.nrows, 0) > kShRows;
             const int rest = __shfl_sync(0xffffffffu, item.pages - item.tile0 * TP, 0);  // pages from the item's first on
-            const int ahead = dual ? 1 : 2, lead = min(ahead, n);
-            // place of K_t and V_t in the producer's order: K_0 (K_1), then V_t, K_(t+ahead) in turn
-            auto place = [&](int t, bool is_v) {
-                if (!is_v && t < ahead) return base + t;
-                const int u = is_v ? t : t - ahead;                    // V_u is behind u V's and the K's that followed them
-                return base + lead + u + min(u, n - lead) + (is_v ? 0u : 1u);
-            };
-            auto acquire = [&](uint32_t at) {
-                const uint32_t sl = at % C::kSlots;
-                ok = warp_wait(&ctl.full[sl], (at / C::kSlots) & 1, abort_flag, p.status);
+            const int ahead = dual ? C::kBufs : 2, lead = min(ahead, n);
+            const int step = dual ? 1 : 2, t0 = dual ? 0 : s;     // the stream's tiles: t0, t0 + step, ...
+            const int nt = t0 < n ? (n - t0 + step - 1) / step : 0;
+            const int bufs = dual ? C::kBufs : 1;
+            // slots in the producers' order: K_0 .. K_(lead-1) alone, then V_t with K_(t+ahead)
+            uint32_t slot = 0, phase = 0;
+            auto go_to = [&](uint32_t at) { slot = at % C::kSlots; phase = (at / C::kSlots) & 1; };
+            auto acquire = [&]() {
+                ok = warp_wait(&ctl.full[slot], phase, abort_flag, p.status);
                 tc_fence_after();
-                return sl;
             };
-            auto release = [&](uint32_t sl) {  // in the wide form a slot is free after two arrivals: one of each stream,
+            auto release = [&]() {             // in the wide form a slot is free after two arrivals: one of each stream,
                 if (!leader) return;           // or both of the only one that reads it
-                tc_commit(smem_u32(&ctl.empty[sl]));
-                if (kWide && !dual) tc_commit(smem_u32(&ctl.empty[sl]));
+                tc_commit(smem_u32(&ctl.empty[slot]));
+                if (kWide && !dual) tc_commit(smem_u32(&ctl.empty[slot]));
             };
-            auto qk = [&](uint32_t sl) {       // whole tile (columns past the last page are not used)
-                const uint32_t b = k_lo + sl * (C::kSlotBytes >> 4);
+            auto qk = [&](int u) {             // whole tile (columns past the last page are not used)
+                const uint32_t b = k_lo + slot * (C::kSlotBytes >> 4), d = sp0 + u * C::kSpCols;
                 if (leader) {
 #pragma unroll
                     for (int k = 0; k < D / 16; ++k)
-                        tc_mma_ss(ts, q_lo + (k >> 2) * (kShRows * 128 >> 4) + (k & 3) * 2, b + (k >> 2) * (TN * 128 >> 4) + (k & 3) * 2,
+                        tc_mma_ss(d, q_lo + (k >> 2) * (kShRows * 128 >> 4) + (k & 3) * 2, b + (k >> 2) * (TN * 128 >> 4) + (k & 3) * 2,
                                   kDescHi, idesc_s, k > 0);
-                    tc_commit(smem_u32(&ctl.s_full[s]));
+                    tc_commit(smem_u32(&ctl.s_full[s][u]));
                 }
             };
             // narrow: one copy of Q, loaded by stream 0 for every item; wide: each stream's own, where it has a tile
-            if (!kWide || dual || s < n) {
+            if (!kWide || nt > 0) {
                 ok = warp_wait(&ctl.q_full[kWide ? s : 0], nq++ & 1, abort_flag, p.status);
                 if (!ok) break;
                 tc_fence_after();
             }
-            if (dual || s < n) {
-                const int step = dual ? 1 : 2, t0 = dual ? 0 : s;
-                uint32_t ks = acquire(place(t0, false));
+            for (int i = 0; i < min(bufs, nt); ++i) {
+                go_to(base + t0 + i * step);
+                acquire();
                 if (!ok) break;
-                qk(ks);
-                release(ks);
-                for (int t = t0; t < n; t += step) {
-                    const uint32_t vs = acquire(place(t, true));
-                    if (!ok) break;
-                    const bool more = t + step < n;
-                    if (more) {                // the next K is usually there: its barrier is looked at ahead of the products
-                        ks = acquire(place(t + step, false));
-                        if (!ok) break;
-                    }
-                    ok = warp_wait(&ctl.p_full[s], np++ & 1, abort_flag, p.status);
-                    if (!ok) break;
-                    tc_fence_after();
-                    const int pages = min(TP, rest - t * TP);
-                    const bool first = t == t0;
-                    const uint32_t b = v_lo + vs * (C::kSlotBytes >> 4);
-                    if (leader) {              // a page is one K step of 16 positions
-                        if (pages == TP) {
-#pragma unroll
-                            for (int k = 0; k < TP; ++k)
-#pragma unroll
-                                for (int c = 0; c < kTerms; ++c)
-                                    tc_mma_ts(to, ts + c * (TN / 2) + k * 8, b + k * (kPage * D * 2 >> 4), kDescHi, idesc_o, !first || k + c > 0);
-                        } else {
-                            for (int k = 0; k < pages; ++k)
-#pragma unroll
-                                for (int c = 0; c < kTerms; ++c)
-                                    tc_mma_ts(to, ts + c * (TN / 2) + k * 8, b + k * (kPage * D * 2 >> 4), kDescHi, idesc_o, !first || k + c > 0);
-                        }
-                    }
-                    // (S of the next tile takes P's place: products of one thread run in order)
-                    if (more) qk(ks);
-                    release(vs);
-                    if (more) release(ks);
-                    if (!more && leader) tc_commit(smem_u32(&ctl.o_full[s]));
-                }
+                qk(i);
+                release();
             }
-            base += 2 * n;
+            go_to(base + lead + t0);
+            for (int i = 0; i < nt && ok; ++i) {
+                const int u = bufs == 2 ? i & 1 : 0;
+                acquire();
+                if (!ok) break;
+                const uint32_t ph = u ? np[1]++ : np[0]++;
+                ok = warp_wait(&ctl.p_full[s][u], ph & 1, abort_flag, p.status);
+                if (!ok) break;
+                tc_fence_after();
+                const int pages = min(TP, rest - (t0 + i * step) * TP);
+                const uint32_t b = v_lo + slot * (C::kSlotBytes >> 4), a = sp0 + u * C::kSpCols;
+                auto product = [&](int k) {    // a page is one K step of 16 positions
+#pragma unroll
+                    for (int c = 0; c < kTerms; ++c)
+                        tc_mma_ts(to, a + c * (TN / 2) + k * 8, b + k * (kPage * D * 2 >> 4), kDescHi, idesc_o, i > 0 || k + c > 0);
+                };
+                if (leader) {
+                    if (pages == TP) {
+#pragma unroll
+                        for (int k = 0; k < TP; ++k) product(k);
+                    } else {
+                        for (int k = 0; k < pages; ++k) product(k);
+                    }
+                }
+                if (i + bufs < nt) {
+                    qk(u);                     // (S takes P's place: products of one thread run in order)
+                } else if (leader) {
+                    tc_commit(smem_u32(&ctl.pv_done[s][u]));
+                }
+                release();
+                slot += step;
+                if (slot >= C::kSlots) { slot -= C::kSlots; phase ^= 1; }
+            }
+            base += lead + n;
         }
         __syncwarp();
     }
@@ -505,10 +513,10 @@ shared_prefix_kernel(const __grid_constant__ SharedParams p, const __grid_consta
         // ============================ softmax warpgroups: one thread per row ============================
         const int s = warp >> 2;                     // stream
         const int tr = tid & (kShRows - 1);          // row of the tile = TMEM lane
-        const uint32_t sp = tmem + ((uint32_t)(warp & 3) << 21) + s * C::kSpCols;
+        const uint32_t sp0 = tmem + ((uint32_t)(warp & 3) << 21) + s * C::kBufs * C::kSpCols;
         const uint32_t oc = tmem + ((uint32_t)(warp & 3) << 21) + C::kO0;
         const float scale = p.scale_log2e;
-        uint32_t ns = 0, no = 0, nj = 0;
+        uint32_t ns[2] = {0, 0}, nd[2] = {0, 0}, nj = 0;  // tiles seen in each buffer, items that ended in it
         bool ok = true;
         for (int x = x0; x < x1 && ok;) {
             const ShItem it = shared_item<TP, C::kRowBlock>(p, pl, x, x1);
@@ -542,22 +550,29 @@ shared_prefix_kernel(const __grid_constant__ SharedParams p, const __grid_consta
             }
             float m = -INFINITY, l = 0.f;  // m in log2 units
             bool fresh = true;
-            for (int t = dual ? 0 : s; t < it.n; t += dual ? 1 : 2) {
-                if (!warp_wait(&ctl.s_full[s], ns++ & 1, abort_flag, p.status)) { ok = false; break; }
+            const int step = dual ? 1 : 2, t0 = dual ? 0 : s, bufs = dual ? C::kBufs : 1;
+            const int nt = (it.n - t0 + step - 1) / step;
+            for (int i = 0; i < nt; ++i) {
+                const int t = t0 + i * step, u = bufs == 2 ? i & 1 : 0;
+                const uint32_t sp = sp0 + u * C::kSpCols;
+                const uint32_t ph = u ? ns[1]++ : ns[0]++;
+                if (!warp_wait(&ctl.s_full[s][u], ph & 1, abort_flag, p.status)) { ok = false; break; }
                 tc_fence_after();
                 if (warp_valid) {
                     const int cols = min(TP, it.pages - (it.tile0 + t) * TP) * kPage;
-                    float v[TN];
+                    float v[TN], mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                    tc_ld32(sp, v);
 #pragma unroll
-                    for (int c = 0; c < TN; c += 32) tc_ld32(sp + c, v + c);
-                    tc_wait_ld();
-                    if (cols < TN) {
+                    for (int c0 = 0; c0 < TN; c0 += 32) {  // the next 32 columns are on their way while these are looked at
+                        tc_wait_ld();
+                        if (c0 + 32 < TN) tc_ld32(sp + c0 + 32, v + c0 + 32);
+                        if (cols < TN) {
 #pragma unroll
-                        for (int c = 0; c < TN; ++c) v[c] = c < cols ? v[c] : -INFINITY;
+                            for (int c = c0; c < c0 + 32; ++c) v[c] = c < cols ? v[c] : -INFINITY;
+                        }
+#pragma unroll
+                        for (int c = c0; c < c0 + 32; ++c) mx[c & 3] = fmaxf(mx[c & 3], v[c]);
                     }
-                    float mx[4] = {v[0], v[1], v[2], v[3]};
-#pragma unroll
-                    for (int c = 4; c < TN; ++c) mx[c & 3] = fmaxf(mx[c & 3], v[c]);
                     const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * scale;
                     // The running maximum only moves when it would grow by more than 2^8: any value near the true one
                     // gives the same quotient, and O in TMEM then rarely has to be scaled.
@@ -565,7 +580,14 @@ shared_prefix_kernel(const __grid_constant__ SharedParams p, const __grid_consta
                         m = top;
                         fresh = false;
                     } else if (__any_sync(0xffffffffu, top > m + 8.f)) {
-                        // S of this tile is complete, so the products of the tiles before it are too: O is at rest
+                        // O has to be at rest.  This buffer's last product is complete (S was made behind it); the other
+                        // buffer's is once its next S is, or at the end once it says so itself.
+                        if (bufs == 2) {
+                            const uint64_t* bar = i + 1 < nt ? &ctl.s_full[s][u ^ 1] : &ctl.pv_done[s][u ^ 1];
+                            const uint32_t at = i + 1 < nt ? (u ? ns[0] : ns[1]) : (u ? nd[0] : nd[1]);
+                            if (!warp_wait(bar, at & 1, abort_flag, p.status)) { ok = false; break; }
+                            tc_fence_after();
+                        }
                         const float mn = top > m + 8.f ? top : m;
                         const float a = m == -INFINITY ? 0.f : ex2(m - mn);
                         m = mn;
@@ -609,10 +631,12 @@ shared_prefix_kernel(const __grid_constant__ SharedParams p, const __grid_consta
                 }
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(smem_u32(&ctl.p_full[s]));
+                if (lane == 0) mbar_arrive(smem_u32(&ctl.p_full[s][u]));
             }
             if (!ok) break;
-            if (!warp_wait(&ctl.o_full[s], no++ & 1, abort_flag, p.status)) { ok = false; break; }
+            ok = warp_wait(&ctl.pv_done[s][0], nd[0]++ & 1, abort_flag, p.status);
+            if (ok && bufs == 2 && nt > 1) ok = warp_wait(&ctl.pv_done[s][1], nd[1]++ & 1, abort_flag, p.status);
+            if (!ok) break;
             tc_fence_after();
             // ---- the item's partial: chunk 0 of a unit in the row's own place, later chunks in the span's ----
             const bool joined = !dual && it.n > 1;
@@ -792,11 +816,11 @@ cudaError_t launch_shared_prefix(const SharedParams& p, const void* kmap, const 
     const bool wide = p.batch * p.group > kShRows;
     if (head_dim == 128) {
         if (wide)
-            return out_bf16 ? launch_shared_t<128, 2, true>(p, kmap, vmap, grid, st, pdl) : launch_shared_t<128, 3, true>(p, kmap, vmap, grid, st, pdl);
+            return out_bf16 ? launch_shared_t<128, 1, true>(p, kmap, vmap, grid, st, pdl) : launch_shared_t<128, 3, true>(p, kmap, vmap, grid, st, pdl);
         return out_bf16 ? launch_shared_t<128, 2, false>(p, kmap, vmap, grid, st, pdl) : launch_shared_t<128, 3, false>(p, kmap, vmap, grid, st, pdl);
     }
     if (wide)
-        return out_bf16 ? launch_shared_t<64, 2, true>(p, kmap, vmap, grid, st, pdl) : launch_shared_t<64, 3, true>(p, kmap, vmap, grid, st, pdl);
+        return out_bf16 ? launch_shared_t<64, 1, true>(p, kmap, vmap, grid, st, pdl) : launch_shared_t<64, 3, true>(p, kmap, vmap, grid, st, pdl);
     return out_bf16 ? launch_shared_t<64, 2, false>(p, kmap, vmap, grid, st, pdl) : launch_shared_t<64, 3, false>(p, kmap, vmap, grid, st, pdl);
 }
 
