@@ -1,23 +1,31 @@
 // Eviction of a paged cache down to a budget, by accumulated attention weight.
 //
-// For every (cache slice, request, kv head) with t > budget positions, the kept set is
+// For every unit (cache slice, request, kv head) with t > budget positions, the kept set is
 //   {0 .. sinks-1}  u  {t-recent .. t-1}  u  the (budget - sinks - recent) heaviest positions between them
 // (ties to the lowest index); K, V and the weights of the kept positions move to 0 .. budget-1 in order of position.
 //
 // 1. evict_select_kernel finds the kept set: a radix select over the order-preserving 32-bit image of the weights (four
 //    8-bit digits, most significant first) gives the lightest kept weight T and how many positions of exactly T
 //    belong to the set; one ordered pass with a prefix sum writes the list of kept positions and compacts the weights.
+//    A unit is a cluster of 1 to 8 CTAs; each holds its part of the weights in shared memory, so that they are read
+//    once, and histograms and counts are added up through distributed shared memory.
 // 2. evict_move_kernel moves the rows in place.  Destination i never lies behind its source (i <= kept[i], both
-//    rising), so a chunk of rows whose sources have all been read may be written: later sources lie behind it.
+//    rising), so a chunk of rows whose sources have all been read may be written: later sources lie behind it.  That
+//    orders the rows of a unit, but not its columns: K and V, and slices of 32 bytes or more of a row, are moved by
+//    CTAs that know nothing of one another.  Rows before the first dropped position stay where they are.
+//
+// Bound by memory: 4 bytes a position once, and 2 x 4 D bytes (read and write) for every row that moves.
 #include "launch_ex.cuh"
+#include "mbar.cuh"
 #include "oda_device.cuh"
 #include "oda_launch.h"
 
 namespace oda {
 
-constexpr int kSelThreads = 1024;
-constexpr int kMoveThreads = 512;
-constexpr int kMovePieces = 8;  // 16-byte pieces a thread holds of one chunk
+constexpr int kSelThreads = 512;
+constexpr int kSelWarps = kSelThreads / 32;
+constexpr int kSelCap = 24576;        // positions a CTA holds (96 KiB: two CTAs per SM)
+constexpr int kMovePieces = 8;        // 16-byte pieces a thread holds of one chunk
 
 // larger weight -> larger key; -0 and +0 are one key, NaN is above everything
 __device__ __forceinline__ uint32_t weight_key(float w)
@@ -27,17 +35,51 @@ __device__ __forceinline__ uint32_t weight_key(float w)
     return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
 }
 
+__device__ __forceinline__ uint32_t cluster_rank()
+{
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_sync(int n)
+{
+    if (n == 1) {
+        __syncthreads();
+        return;
+    }
+    asm volatile("barrier.cluster.arrive.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+}
+// a word of the same variable in CTA `rank` of the cluster
+__device__ __forceinline__ uint32_t cluster_peek(const uint32_t* var, uint32_t rank)
+{
+    uint32_t a, v;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_u32(var)), "r"(rank));
+    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
+    return v;
+}
+
+struct SelShared {
+    uint32_t hist[3][256];            // this CTA's digits, a buffer per pass in turn: one is counted in, one may still be
+                                      // read by other CTAs, one is cleared
+    uint32_t total[256];              // the cluster's
+    uint32_t counts[2][2];            // by parity of the round: positions heavier than T, and of weight T
+    uint32_t wcount[kSelWarps];       // per warp: heavier | equal << 16
+    uint32_t prefix, left;
+};
+
 __global__ void __launch_bounds__(kSelThreads)
-evict_select_kernel(const __grid_constant__ EvictParams p)
+evict_select_kernel(const __grid_constant__ EvictParams p, const int nc)
 {
     griddep_wait();
     griddep_launch_dependents();
-    __shared__ uint32_t hist[256];
-    __shared__ uint32_t s_prefix, s_left;
-    __shared__ uint32_t wsum[kSelThreads / 32];
+    extern __shared__ float part[];   // this CTA's positions of the round
+    __shared__ SelShared sh;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int unit = blockIdx.x;  // (slice, request, head)
+    const int rank = nc > 1 ? (int)cluster_rank() : 0;
+    const int unit = blockIdx.x / nc;
     const int g = unit % p.num_kv_heads, b = (unit / p.num_kv_heads) % p.batch, slice = unit / (p.num_kv_heads * p.batch);
+    // (everything that leaves early is the same in all CTAs of a cluster)
     if (p.mask && !p.mask[b]) return;
     const int t = p.seq_lens[b];
     const size_t max_pos = (size_t)p.max_blocks_per_seq * kPage;
@@ -45,30 +87,67 @@ evict_select_kernel(const __grid_constant__ EvictParams p)
         if (tid == 0) atomicOr(p.status, kStatusBadSeqLen);
         return;
     }
-    int32_t* kept = p.kept + (size_t)unit * p.budget;
     const int n = p.budget;
+    int32_t* kept = p.kept + (size_t)unit * n;
     if (t <= n) {  // nothing to drop
-        for (int i = tid; i < n; i += kSelThreads) kept[i] = i < t ? i : -1;
+        for (int i = rank * kSelThreads + tid; i < n; i += nc * kSelThreads) kept[i] = i < t ? i : -1;
         return;
     }
     float* w = p.weights + (((size_t)slice * p.max_batch + b) * p.num_kv_heads + g) * max_pos;
     const int lo = p.sinks, hi = t - p.recent;  // candidates
-    uint32_t left = (uint32_t)(n - p.sinks - p.recent);  // how many of them stay (less than hi - lo)
+    const bool any = n > p.sinks + p.recent;
+    // positions of a CTA in one round: all of them where they fit, else as many as fit
+    const int per = min(((t + nc - 1) / nc + 31) / 32 * 32, p.part_cap);
+    const int rounds = (int)(((long long)t + (long long)per * nc - 1) / ((long long)per * nc));
+    int* first = p.first + unit;                // first dropped position
+    if (rank == 0 && tid == 0) *first = 0x7fffffff;
+    auto load_part = [&](int r) {
+        const long long i0 = ((long long)r * nc + rank) * per;
+        const int m = (int)max(0ll, min((long long)per, t - i0));
+        for (int i = tid; i < m; i += 4 * kSelThreads) {
+            float v[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[k] = i + k * kSelThreads < m ? __ldcg(w + i0 + i + k * kSelThreads) : 0.f;
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (i + k * kSelThreads < m) part[i + k * kSelThreads] = v[k];
+        }
+        return m;
+    };
+    if (tid < 256) sh.hist[0][tid] = 0;
+    int m = 0;
+    if (rounds == 1) m = load_part(0);
+    __syncthreads();
+    uint32_t left = (uint32_t)(n - p.sinks - p.recent);  // how many of the candidates stay (fewer than there are)
     uint32_t prefix = 0;
-    if (left > 0) {
-        for (int shift = 24; shift >= 0; shift -= 8) {
-            for (int i = tid; i < 256; i += kSelThreads) hist[i] = 0;
-            __syncthreads();
-            const uint32_t above = shift == 24 ? 0u : 0xffffffffu << (shift + 8);
-            for (int i = lo + tid; i < hi; i += kSelThreads) {
-                const uint32_t k = weight_key(w[i]);
-                if ((k & above) == prefix) atomicAdd(&hist[(k >> shift) & 255u], 1u);
+    if (any) {
+        for (int pass = 0; pass < 4; ++pass) {
+            const int shift = 24 - 8 * pass, cur = pass % 3;
+            const uint32_t above = pass == 0 ? 0u : 0xffffffffu << (shift + 8);
+            auto count = [&](float v) {
+                const uint32_t k = weight_key(v);
+                if ((k & above) == prefix) atomicAdd(&sh.hist[cur][(k >> shift) & 255u], 1u);
+            };
+            if (rounds == 1) {
+                const int i0 = rank * per;
+                const int from = max(0, lo - i0), to = min(m, hi - i0);
+                for (int i = from + tid; i < to; i += kSelThreads) count(part[i]);
+            } else {
+                for (int i = lo + rank * kSelThreads + tid; i < hi; i += nc * kSelThreads) count(__ldcg(w + i));
+            }
+            if (tid < 256) sh.hist[(pass + 1) % 3][tid] = 0;
+            cluster_sync(nc);
+            if (tid < 256) {
+                uint32_t sum = 0;
+                if (nc == 1) sum = sh.hist[cur][tid];
+                else for (int r = 0; r < nc; ++r) sum += cluster_peek(&sh.hist[cur][tid], r);
+                sh.total[tid] = sum;
             }
             __syncthreads();
             if (warp == 0) {  // the digit in which the count from above reaches `left`
                 uint32_t c[8], sum = 0;
 #pragma unroll
-                for (int k = 0; k < 8; ++k) { c[k] = hist[255 - (lane * 8 + k)]; sum += c[k]; }
+                for (int k = 0; k < 8; ++k) { c[k] = sh.total[255 - (lane * 8 + k)]; sum += c[k]; }
                 uint32_t x = sum;
                 for (int o = 1; o < 32; o <<= 1) {
                     const uint32_t y = __shfl_up_sync(0xffffffffu, x, o);
@@ -79,8 +158,8 @@ evict_select_kernel(const __grid_constant__ EvictParams p)
 #pragma unroll
                     for (int k = 0; k < 8; ++k) {
                         if (before < left && before + c[k] >= left) {
-                            s_prefix = prefix | ((uint32_t)(255 - (lane * 8 + k)) << shift);
-                            s_left = left - before;
+                            sh.prefix = prefix | ((uint32_t)(255 - (lane * 8 + k)) << shift);
+                            sh.left = left - before;
                             break;
                         }
                         before += c[k];
@@ -88,64 +167,100 @@ evict_select_kernel(const __grid_constant__ EvictParams p)
                 }
             }
             __syncthreads();
-            prefix = s_prefix;
-            left = s_left;
+            prefix = sh.prefix;
+            left = sh.left;
         }
     }
-    // ordered pass: heavier than T, or T itself while `left` of them last
+    // ordered pass: heavier than T, or T itself while `left` of them last.  A warp owns a run of its CTA's part: it
+    // counts, the counts before it are added up, and it goes over the run again with the places known.
     const uint32_t T = prefix;
-    const bool any = n > p.sinks + p.recent;
     uint32_t base_gt = 0, base_eq = 0;
-    for (int i0 = 0; i0 < t; i0 += kSelThreads) {
-        const int i = i0 + tid;
-        float val = 0.f;
-        uint32_t gt = 0, eq = 0;
-        if (i < t) {
-            val = w[i];
-            const uint32_t k = weight_key(val);
-            const bool fixed = i < lo || i >= hi;
-            gt = fixed || (any && k > T);
-            eq = !fixed && any && k == T;
+    for (int r = 0; r < rounds; ++r) {
+        if (rounds > 1) {
+            m = load_part(r);
+            __syncthreads();
         }
-        uint32_t x = gt | (eq << 16);  // at most 1024 of each in a block
-        for (int o = 1; o < 32; o <<= 1) {
-            const uint32_t y = __shfl_up_sync(0xffffffffu, x, o);
-            if (lane >= o) x += y;
-        }
-        if (lane == 31) wsum[warp] = x;
-        __syncthreads();
-        if (warp == 0) {
-            uint32_t y = wsum[lane];
-            for (int o = 1; o < 32; o <<= 1) {
-                const uint32_t z = __shfl_up_sync(0xffffffffu, y, o);
-                if (lane >= o) y += z;
+        const long long i0 = ((long long)r * nc + rank) * per;
+        const int run = per / 32 / kSelWarps * 32 + 32;            // positions of one warp
+        const int j0 = warp * run, j1 = min(m, j0 + run);
+        auto classes = [&](int j, uint32_t& gt, uint32_t& eq) {    // of positions j + lane
+            bool is_gt = false, is_eq = false;
+            if (j + lane < j1) {
+                const long long i = i0 + j + lane;
+                const uint32_t k = weight_key(part[j + lane]);
+                const bool fixed = i < lo || i >= hi;
+                is_gt = fixed || (any && k > T);
+                is_eq = !fixed && any && k == T;
             }
-            wsum[lane] = y;
+            gt = __ballot_sync(0xffffffffu, is_gt);
+            eq = __ballot_sync(0xffffffffu, is_eq);
+        };
+        uint32_t ngt = 0, neq = 0;
+        for (int j = j0; j < j1; j += 32) {
+            uint32_t gt, eq;
+            classes(j, gt, eq);
+            ngt += __popc(gt);
+            neq += __popc(eq);
         }
+        if (lane == 0) sh.wcount[warp] = ngt | (neq << 16);        // (at most 24,576 of each)
         __syncthreads();
-        const uint32_t incl = x + (warp ? wsum[warp - 1] : 0);
-        const uint32_t gts = base_gt + (incl & 0xffffu) - gt, eqs = base_eq + (incl >> 16) - eq;
-        if (gt || (eq && eqs < left)) {
-            const uint32_t dst = gts + min(eqs, left);
-            kept[dst] = i;
-            w[dst] = val;  // dst <= i, and every weight up to this block's end has been read
+        uint32_t gts = base_gt, eqs = base_eq, all_gt = 0, all_eq = 0;
+        for (int k = 0; k < kSelWarps; ++k) {
+            const uint32_t c = sh.wcount[k];
+            if (k < warp) { gts += c & 0xffffu; eqs += c >> 16; }
+            all_gt += c & 0xffffu;
+            all_eq += c >> 16;
         }
-        base_gt += wsum[31] & 0xffffu;
-        base_eq += wsum[31] >> 16;
-        __syncthreads();
+        if (nc > 1) {
+            if (tid == 0) { sh.counts[r & 1][0] = all_gt; sh.counts[r & 1][1] = all_eq; }
+            cluster_sync(nc);                                      // all parts of the round are in shared memory
+            uint32_t sum_gt = 0, sum_eq = 0;
+            for (int k = 0; k < nc; ++k) {
+                const uint32_t cg = cluster_peek(&sh.counts[r & 1][0], k), ce = cluster_peek(&sh.counts[r & 1][1], k);
+                if (k < rank) { gts += cg; eqs += ce; }
+                sum_gt += cg;
+                sum_eq += ce;
+            }
+            base_gt += sum_gt;
+            base_eq += sum_eq;
+        } else {
+            base_gt += all_gt;
+            base_eq += all_eq;
+        }
+        bool dropped = false;
+        for (int j = j0; j < j1; j += 32) {
+            uint32_t gt, eq;
+            classes(j, gt, eq);
+            const uint32_t below = (1u << lane) - 1u;
+            const uint32_t my_gt = gts + __popc(gt & below), my_eq = eqs + __popc(eq & below);
+            const bool keep = ((gt >> lane) & 1u) || (((eq >> lane) & 1u) && my_eq < left);
+            if (keep) {
+                const uint32_t dst = my_gt + min(my_eq, left);
+                kept[dst] = (int32_t)(i0 + j + lane);
+                w[dst] = part[j + lane];   // dst is not behind its source, and every weight of the round has been read
+            }
+            const uint32_t gone = __ballot_sync(0xffffffffu, !keep && j + lane < j1);
+            if (gone && !dropped) {
+                dropped = true;
+                if (lane == 0) atomicMin(first, (int)(i0 + j + __ffs(gone) - 1));
+            }
+            gts += __popc(gt);
+            eqs += __popc(eq);
+        }
+        __syncthreads();                   // part and wcount are used again
     }
-    for (int i = n + tid; i < t; i += kSelThreads) w[i] = 0.f;
+    cluster_sync(nc);                      // nobody leaves while others read its counts; all kept weights are written
+    for (int i = n + rank * kSelThreads + tid; i < t; i += nc * kSelThreads) w[i] = 0.f;
 }
 
-template <int D>
-__global__ void __launch_bounds__(kMoveThreads)
+// grid: (unit, K or V and slice of the row).  kPieces 16-byte pieces of a row are one CTA's.
+template <int kPieces>
+__global__ void __launch_bounds__(1024)
 evict_move_kernel(const __grid_constant__ EvictParams p)
 {
     griddep_wait();
     griddep_launch_dependents();
-    constexpr int kRowPieces = D / 8;                                  // 16-byte pieces of one K (or V) row
-    constexpr int kRows = kMoveThreads * kMovePieces / (2 * kRowPieces);  // rows of one chunk, K and V
-    const int tid = threadIdx.x;
+    const int tid = threadIdx.x, nth = blockDim.x;
     const int unit = blockIdx.x;
     const int g = unit % p.num_kv_heads, b = (unit / p.num_kv_heads) % p.batch, slice = unit / (p.num_kv_heads * p.batch);
     const int t = p.seq_lens[b];
@@ -153,45 +268,39 @@ evict_move_kernel(const __grid_constant__ EvictParams p)
     const bool work = (!p.mask || p.mask[b]) && t > n && (size_t)t <= (size_t)p.max_blocks_per_seq * kPage;
     if (work) {
         const int32_t* kept = p.kept + (size_t)unit * n;
-        // kept[i] - i never falls: the rows that stay where they are come first
-        int i0 = 0, i1 = n;
-        while (i0 < i1) {
-            const int mid = (i0 + i1) >> 1;
-            if (kept[mid] == mid) i0 = mid + 1; else i1 = mid;
-        }
         const int32_t* table = p.block_table + (size_t)b * p.max_blocks_per_seq;
-        const size_t unit_off = (size_t)slice * p.kv_layer_stride + (size_t)g * p.kv_head_stride;
-        auto row = [&](int pos) {
-            return unit_off + (size_t)table[pos / kPage] * p.kv_block_stride + (size_t)(pos % kPage) * p.kv_token_stride;
-        };
-        for (; i0 < n; i0 += kRows) {
+        const int c = tid % kPieces, r0 = tid / kPieces, rows = nth / kPieces;  // rows of one of the thread's pieces
+        __nv_bfloat16* base = ((blockIdx.y & 1) ? p.v : p.k) + (size_t)slice * p.kv_layer_stride + (size_t)g * p.kv_head_stride +
+                              (size_t)((blockIdx.y >> 1) * kPieces + c) * 8;
+        auto row = [&](int pos) { return base + (size_t)table[pos / kPage] * p.kv_block_stride + (size_t)(pos % kPage) * p.kv_token_stride; };
+        int src[kMovePieces];
+        int i0 = min(p.first[unit], n);
+#pragma unroll
+        for (int k = 0; k < kMovePieces; ++k) {
+            const int i = i0 + r0 + k * rows;
+            src[k] = i < n ? kept[i] : 0;
+        }
+        for (; i0 < n; i0 += kMovePieces * rows) {
             uint4 x[kMovePieces];
 #pragma unroll
-            for (int k = 0; k < kMovePieces; ++k) {
-                const int e = tid + k * kMoveThreads;
-                const int r = e / (2 * kRowPieces), c = e % (2 * kRowPieces);
-                if (i0 + r < n) {
-                    const __nv_bfloat16* base = c < kRowPieces ? p.k : p.v;
-                    x[k] = *reinterpret_cast<const uint4*>(base + row(kept[i0 + r]) + (size_t)(c % kRowPieces) * 8);
-                }
+            for (int k = 0; k < kMovePieces; ++k)
+                if (i0 + r0 + k * rows < n) x[k] = *reinterpret_cast<const uint4*>(row(src[k]));
+#pragma unroll
+            for (int k = 0; k < kMovePieces; ++k) {  // the next chunk's sources, while the rows are on their way
+                const int i = i0 + r0 + (k + kMovePieces) * rows;
+                src[k] = i < n ? kept[i] : 0;
             }
             __syncthreads();
 #pragma unroll
-            for (int k = 0; k < kMovePieces; ++k) {
-                const int e = tid + k * kMoveThreads;
-                const int r = e / (2 * kRowPieces), c = e % (2 * kRowPieces);
-                if (i0 + r < n) {
-                    __nv_bfloat16* base = c < kRowPieces ? p.k : p.v;
-                    *reinterpret_cast<uint4*>(base + row(i0 + r) + (size_t)(c % kRowPieces) * 8) = x[k];
-                }
-            }
+            for (int k = 0; k < kMovePieces; ++k)
+                if (i0 + r0 + k * rows < n) *reinterpret_cast<uint4*>(row(i0 + r0 + k * rows)) = x[k];
             __syncthreads();
         }
     }
     // the CTA that comes last shortens the requests: nobody reads their lengths any more
     if (tid == 0) {
         __threadfence();
-        if (atomicAdd(p.done, 1) == (int)gridDim.x - 1) {
+        if (atomicAdd(p.done, 1) == (int)(gridDim.x * gridDim.y) - 1) {
             *p.done = 0;
             for (int r = 0; r < p.batch; ++r)
                 if ((!p.mask || p.mask[r]) && p.seq_lens[r] > n && (size_t)p.seq_lens[r] <= (size_t)p.max_blocks_per_seq * kPage)
@@ -200,13 +309,47 @@ evict_move_kernel(const __grid_constant__ EvictParams p)
     }
 }
 
-cudaError_t launch_evict(const EvictParams& p, int head_dim, cudaStream_t st, bool pdl)
+cudaError_t launch_evict(const EvictParams& args, int head_dim, int num_sms, cudaStream_t st, bool pdl)
 {
-    const unsigned units = (unsigned)(p.num_slices * p.batch * p.num_kv_heads);
-    cudaError_t e = launch_ex(evict_select_kernel, dim3(units), dim3(kSelThreads), 0, st, pdl, p);
+    EvictParams p = args;
+    const long long units = (long long)p.num_slices * p.batch * p.num_kv_heads;
+    const long long max_pos = (long long)p.max_blocks_per_seq * kPage;
+    // as many CTAs per unit as give every SM two, or as its positions need to fit shared memory
+    int nc = 1;
+    while (nc < 8 && (units * nc < 2 * num_sms || max_pos > (long long)kSelCap * nc) && max_pos > 1024 * nc) nc *= 2;
+    p.part_cap = (int)((max_pos + nc - 1) / nc + 31) / 32 * 32;
+    if (p.part_cap > kSelCap) p.part_cap = kSelCap;
+    const int smem = p.part_cap * (int)sizeof(float);
+    cudaError_t e = cudaFuncSetAttribute(evict_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSelCap * (int)sizeof(float));
     if (e != cudaSuccess) return e;
-    if (head_dim == 128) return launch_ex(evict_move_kernel<128>, dim3(units), dim3(kMoveThreads), 0, st, pdl, p);
-    return launch_ex(evict_move_kernel<64>, dim3(units), dim3(kMoveThreads), 0, st, pdl, p);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(units * nc));
+    cfg.blockDim = dim3(kSelThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = nc;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = pdl ? 2 : 1;
+    e = cudaLaunchKernelEx(&cfg, evict_select_kernel, p, nc);
+    if (e != cudaSuccess) return e;
+    // whole rows of K and of V where that fills the SMs, else narrower slices (not below 32 bytes: a DRAM sector)
+    int pieces = head_dim / 8, slices = 1;
+    while (pieces > 2 && units * 2 * slices < 3 * num_sms) {
+        pieces /= 2;
+        slices *= 2;
+    }
+    const dim3 grid((unsigned)units, 2 * slices), block(units * 2 * slices < 3 * num_sms ? 1024 : 256);
+    switch (pieces) {
+        case 16: return launch_ex(evict_move_kernel<16>, grid, block, 0, st, pdl, p);
+        case 8: return launch_ex(evict_move_kernel<8>, grid, block, 0, st, pdl, p);
+        case 4: return launch_ex(evict_move_kernel<4>, grid, block, 0, st, pdl, p);
+        default: return launch_ex(evict_move_kernel<2>, grid, block, 0, st, pdl, p);
+    }
 }
 
 }  // namespace oda

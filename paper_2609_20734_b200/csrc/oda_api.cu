@@ -23,7 +23,7 @@ constexpr size_t kAlign = 256;
 size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
 
 struct WsLayout {
-    size_t status, layers, tickets, head_partial, head_pre, head_rb_tickets, sm_claims, sm_bytes, cum_share, partials;
+    size_t status, layers, tickets, head_partial, head_pre, head_rb_tickets, sm_claims, sm_bytes, cum_share, evict_first, partials;
     size_t st_q_local, st_q_full, st_feat, st_override, st_out, st_lse, st_scores, st_logits, st_flags, own_lse;
     size_t total;
 };
@@ -102,6 +102,7 @@ void compute_layout(oda_ctx* c)
     w.sm_claims = take(1024 * sizeof(int32_t));
     w.sm_bytes = take(2 * 1024 * sizeof(unsigned long long));
     w.cum_share = take((kMaxGrid + 1) * sizeof(uint16_t));
+    w.evict_first = take((size_t)c->phys_layers * B * f.num_kv_heads * sizeof(int32_t));
     w.partials = take((size_t)c->max_items * std::max<size_t>(c->group * (D + kPartHdr), tma_partial_slot_floats()) * sizeof(float));
     w.st_q_local = take(L * B * Hq * D * 2);
     w.st_q_full = take(L * B * Hq * D * 2);
@@ -1211,6 +1212,7 @@ oda_status_t oda_evict(oda_ctx_t* c, int32_t batch, float* weights, void* k, voi
     p.kept = kept;
     p.status = reinterpret_cast<int32_t*>(c->ws + c->lay.status);
     p.done = reinterpret_cast<int32_t*>(c->ws + c->lay.status + 32);
+    p.first = reinterpret_cast<int32_t*>(c->ws + c->lay.evict_first);
     p.kv_layer_stride = f.kv_layer_stride;
     p.kv_block_stride = f.kv_block_stride;
     p.kv_token_stride = f.kv_token_stride;
@@ -1223,7 +1225,7 @@ oda_status_t oda_evict(oda_ctx_t* c, int32_t batch, float* weights, void* k, voi
     p.budget = budget;
     p.sinks = sinks;
     p.recent = recent;
-    cudaError_t e = launch_evict(p, f.head_dim, static_cast<cudaStream_t>(stream), c->use_pdl);
+    cudaError_t e = launch_evict(p, f.head_dim, c->num_sms, static_cast<cudaStream_t>(stream), c->use_pdl);
     if (e != cudaSuccess) return cuda_fail(c, e, "eviction launch");
     c->launches += 2;
     return ODA_OK;

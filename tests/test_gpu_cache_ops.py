@@ -233,7 +233,7 @@ def test_evict_layouts_masks_slices(D, Hkv, layout):
     check_evict(prob, w, 1024, 0, 1, with_kept=False, kv_index=[0, 1, 0])
 
 
-@pytest.mark.parametrize("t,budget", [(2053, 2052), (4097, 4096), (9000, 8999), (30000, 17), (70000, 33333)])
+@pytest.mark.parametrize("t,budget", [(2053, 2052), (4097, 4096), (9000, 8999), (30000, 17), (70000, 33333), (300001, 100000)])
 def test_evict_lengths(t, budget):
     """One position too many, and long histories (few units: one unit is worked on by several CTAs)."""
     prob = make_problem(13, 1, 1, 2, 1, 128, [t])
