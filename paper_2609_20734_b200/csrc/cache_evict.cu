@@ -10,9 +10,9 @@
 //    A unit is a cluster of 1 to 8 CTAs; each holds its part of the weights in shared memory, so that they are read
 //    once, and histograms and counts are added up through distributed shared memory.
 // 2. evict_move_kernel moves the rows in place.  Destination i never lies behind its source (i <= kept[i], both
-//    rising), so a chunk of rows whose sources have all been read may be written: later sources lie behind it.  That
-//    orders the rows of a unit, but not its columns: K and V, and slices of 32 bytes or more of a row, are moved by
-//    CTAs that know nothing of one another.  Rows before the first dropped position stay where they are.
+//    rising), so a chunk of rows whose sources have all been read may be written: later sources lie behind it.  K and V
+//    are moved by CTAs that know nothing of one another; where that leaves SMs idle, 2 to 8 CTAs in a cluster move a
+//    chunk together.  Rows before the first dropped position stay where they are.
 //
 // Bound by memory: 4 bytes a position once, and 2 x 4 D bytes (read and write) for every row that moves.
 #include "launch_ex.cuh"
@@ -24,8 +24,10 @@ namespace oda {
 
 constexpr int kSelThreads = 512;
 constexpr int kSelWarps = kSelThreads / 32;
-constexpr int kSelCap = 24576;        // positions a CTA holds (96 KiB: two CTAs per SM)
-constexpr int kMovePieces = 8;        // 16-byte pieces a thread holds of one chunk
+constexpr int kSelCap = 24576;        // positions a CTA is meant to hold (96 KiB: two CTAs per SM)
+constexpr int kSelMost = 47104;       // and at most (184 KiB; longer parts are worked through in rounds)
+constexpr int kCopies = 8;            // of a CTA's histogram: lanes that count the same digit (most weights share a few
+                                      // exponents) rarely meet in one word
 
 // larger weight -> larger key; -0 and +0 are one key, NaN is above everything
 __device__ __forceinline__ uint32_t weight_key(float w)
@@ -55,13 +57,14 @@ __device__ __forceinline__ uint32_t cluster_peek(const uint32_t* var, uint32_t r
 {
     uint32_t a, v;
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_u32(var)), "r"(rank));
-    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
+    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(a));
     return v;
 }
 
 struct SelShared {
-    uint32_t hist[3][256];            // this CTA's digits, a buffer per pass in turn: one is counted in, one may still be
-                                      // read by other CTAs, one is cleared
+    uint32_t hist[kCopies][256 + 4];
+    uint32_t sum[3][256];             // this CTA's digits, a buffer per pass in turn: one is written, one may still be
+                                      // read by other CTAs
     uint32_t total[256];              // the cluster's
     uint32_t counts[2][2];            // by parity of the round: positions heavier than T, and of weight T
     uint32_t wcount[kSelWarps];       // per warp: heavier | equal << 16
@@ -114,7 +117,8 @@ evict_select_kernel(const __grid_constant__ EvictParams p, const int nc)
         }
         return m;
     };
-    if (tid < 256) sh.hist[0][tid] = 0;
+    if (tid < 256)
+        for (int k = 0; k < kCopies; ++k) sh.hist[k][tid] = 0;
     int m = 0;
     if (rounds == 1) m = load_part(0);
     __syncthreads();
@@ -122,26 +126,45 @@ evict_select_kernel(const __grid_constant__ EvictParams p, const int nc)
     uint32_t prefix = 0;
     if (any) {
         for (int pass = 0; pass < 4; ++pass) {
-            const int shift = 24 - 8 * pass, cur = pass % 3;
+            const int shift = 24 - 8 * pass;
             const uint32_t above = pass == 0 ? 0u : 0xffffffffu << (shift + 8);
-            auto count = [&](float v) {
+            uint32_t* hist = sh.hist[lane % kCopies];
+            // weights of 0 (positions nobody looked at) are one key and may be most of them: a warp adds them at once
+            auto count = [&](float v, bool there) {
                 const uint32_t k = weight_key(v);
-                if ((k & above) == prefix) atomicAdd(&sh.hist[cur][(k >> shift) & 255u], 1u);
+                const bool in = there && (k & above) == prefix;
+                const uint32_t zeros = __ballot_sync(0xffffffffu, in && v == 0.f);
+                if (in && v != 0.f) atomicAdd(&hist[(k >> shift) & 255u], 1u);
+                if (zeros && lane == 0) atomicAdd(&hist[(0x80000000u >> shift) & 255u], (uint32_t)__popc(zeros));
             };
             if (rounds == 1) {
                 const int i0 = rank * per;
                 const int from = max(0, lo - i0), to = min(m, hi - i0);
-                for (int i = from + tid; i < to; i += kSelThreads) count(part[i]);
+                for (int i = from + warp * 32; i < to; i += kSelThreads) count(i + lane < to ? part[i + lane] : 0.f, i + lane < to);
             } else {
-                for (int i = lo + rank * kSelThreads + tid; i < hi; i += nc * kSelThreads) count(__ldcg(w + i));
+                for (int i = lo + (rank * kSelWarps + warp) * 32; i < hi; i += nc * kSelThreads)
+                    count(i + lane < hi ? __ldcg(w + i + lane) : 0.f, i + lane < hi);
             }
-            if (tid < 256) sh.hist[(pass + 1) % 3][tid] = 0;
-            cluster_sync(nc);
+            __syncthreads();
             if (tid < 256) {
                 uint32_t sum = 0;
-                if (nc == 1) sum = sh.hist[cur][tid];
-                else for (int r = 0; r < nc; ++r) sum += cluster_peek(&sh.hist[cur][tid], r);
-                sh.total[tid] = sum;
+#pragma unroll
+                for (int k = 0; k < kCopies; ++k) {
+                    sum += sh.hist[k][tid];
+                    sh.hist[k][tid] = 0;
+                }
+                (nc == 1 ? sh.total : sh.sum[pass % 3])[tid] = sum;
+            }
+            if (nc > 1) {
+                cluster_sync(nc);
+                if (tid < 256) {
+                    uint32_t c[8], sum = 0;
+#pragma unroll
+                    for (int r = 0; r < 8; ++r) c[r] = r < nc ? cluster_peek(&sh.sum[pass % 3][tid], r) : 0u;
+#pragma unroll
+                    for (int r = 0; r < 8; ++r) sum += c[r];
+                    sh.total[tid] = sum;
+                }
             }
             __syncthreads();
             if (warp == 0) {  // the digit in which the count from above reaches `left`
@@ -214,12 +237,17 @@ evict_select_kernel(const __grid_constant__ EvictParams p, const int nc)
         if (nc > 1) {
             if (tid == 0) { sh.counts[r & 1][0] = all_gt; sh.counts[r & 1][1] = all_eq; }
             cluster_sync(nc);                                      // all parts of the round are in shared memory
-            uint32_t sum_gt = 0, sum_eq = 0;
-            for (int k = 0; k < nc; ++k) {
-                const uint32_t cg = cluster_peek(&sh.counts[r & 1][0], k), ce = cluster_peek(&sh.counts[r & 1][1], k);
-                if (k < rank) { gts += cg; eqs += ce; }
-                sum_gt += cg;
-                sum_eq += ce;
+            uint32_t cg[8], ce[8], sum_gt = 0, sum_eq = 0;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                cg[k] = k < nc ? cluster_peek(&sh.counts[r & 1][0], k) : 0u;
+                ce[k] = k < nc ? cluster_peek(&sh.counts[r & 1][1], k) : 0u;
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                if (k < rank) { gts += cg[k]; eqs += ce[k]; }
+                sum_gt += cg[k];
+                sum_eq += ce[k];
             }
             base_gt += sum_gt;
             base_eq += sum_eq;
@@ -253,48 +281,90 @@ evict_select_kernel(const __grid_constant__ EvictParams p, const int nc)
     for (int i = n + rank * kSelThreads + tid; i < t; i += nc * kSelThreads) w[i] = 0.f;
 }
 
-// grid: (unit, K or V and slice of the row).  kPieces 16-byte pieces of a row are one CTA's.
-template <int kPieces>
-__global__ void __launch_bounds__(1024)
-evict_move_kernel(const __grid_constant__ EvictParams p)
+// grid: (unit x CTAs of its cluster, K or V).  kRowPieces: 16-byte pieces of a row.  Chunks of rows run through a ring of
+// kMoveStages in shared memory (each thread copies, and later stores, its own pieces of every chunk): the loads of two
+// chunks are on their way while one is stored, which registers alone did not hold (480 us instead of 380 for 2.1 GB).
+constexpr int kMoveStages = 3;
+template <bool kCluster>
+struct MoveCfg {
+    static constexpr int kThreads = kCluster ? 512 : 256;
+    static constexpr int kPieces = kCluster ? 8 : 4;      // a thread's in one chunk
+    static constexpr int kStageBytes = kThreads * kPieces * 16;
+    static constexpr int kSmem = kMoveStages * kStageBytes;
+};
+
+template <int kRowPieces, bool kCluster>
+__global__ void __launch_bounds__(MoveCfg<kCluster>::kThreads, kCluster ? 1 : 4)
+evict_move_kernel(const __grid_constant__ EvictParams p, const int nc)
 {
     griddep_wait();
     griddep_launch_dependents();
-    const int tid = threadIdx.x, nth = blockDim.x;
-    const int unit = blockIdx.x;
+    using C = MoveCfg<kCluster>;
+    extern __shared__ __align__(16) uint4 ring[];         // [stage][piece][thread]
+    constexpr int kRows = C::kThreads / kRowPieces;       // rows of one piece of every thread
+    constexpr int kChunk = C::kPieces * kRows;            // a CTA's rows of a chunk
+    const int tid = threadIdx.x;
+    const int unit = blockIdx.x / nc, rank = blockIdx.x - unit * nc;
     const int g = unit % p.num_kv_heads, b = (unit / p.num_kv_heads) % p.batch, slice = unit / (p.num_kv_heads * p.batch);
     const int t = p.seq_lens[b];
     const int n = p.budget;
     const bool work = (!p.mask || p.mask[b]) && t > n && (size_t)t <= (size_t)p.max_blocks_per_seq * kPage;
-    if (work) {
+    const int first = work ? min(p.first[unit], n) : n;
+    if (first < n) {
         const int32_t* kept = p.kept + (size_t)unit * n;
         const int32_t* table = p.block_table + (size_t)b * p.max_blocks_per_seq;
-        const int c = tid % kPieces, r0 = tid / kPieces, rows = nth / kPieces;  // rows of one of the thread's pieces
-        __nv_bfloat16* base = ((blockIdx.y & 1) ? p.v : p.k) + (size_t)slice * p.kv_layer_stride + (size_t)g * p.kv_head_stride +
-                              (size_t)((blockIdx.y >> 1) * kPieces + c) * 8;
-        auto row = [&](int pos) { return base + (size_t)table[pos / kPage] * p.kv_block_stride + (size_t)(pos % kPage) * p.kv_token_stride; };
-        int src[kMovePieces];
-        int i0 = min(p.first[unit], n);
+        __nv_bfloat16* base = (blockIdx.y ? p.v : p.k) + (size_t)slice * p.kv_layer_stride + (size_t)g * p.kv_head_stride +
+                              (size_t)(tid % kRowPieces) * 8;
+        auto row = [&](int blk, int pos) { return base + (size_t)blk * p.kv_block_stride + (size_t)(pos % kPage) * p.kv_token_stride; };
+        const int step = nc * kChunk;                     // rows of a chunk
+        const int mine = first + rank * kChunk + tid / kRowPieces;  // this thread's first row of chunk 0
+        const int chunks = (n - first + step - 1) / step;
+        int src[C::kPieces];
+        // Places are looked up together and unconditionally (a row that is not there stands for the last one): one
+        // latency for all of them, not one each.
+        auto list = [&](int c) {
 #pragma unroll
-        for (int k = 0; k < kMovePieces; ++k) {
-            const int i = i0 + r0 + k * rows;
-            src[k] = i < n ? kept[i] : 0;
-        }
-        for (; i0 < n; i0 += kMovePieces * rows) {
-            uint4 x[kMovePieces];
+            for (int k = 0; k < C::kPieces; ++k) src[k] = kept[min(mine + min(c, chunks) * step + k * kRows, n - 1)];
+        };
+        auto load = [&](int c) {                          // src is chunk c's list
+            if (c < chunks) {
+                int blk[C::kPieces];
 #pragma unroll
-            for (int k = 0; k < kMovePieces; ++k)
-                if (i0 + r0 + k * rows < n) x[k] = *reinterpret_cast<const uint4*>(row(src[k]));
+                for (int k = 0; k < C::kPieces; ++k) blk[k] = table[src[k] / kPage];
 #pragma unroll
-            for (int k = 0; k < kMovePieces; ++k) {  // the next chunk's sources, while the rows are on their way
-                const int i = i0 + r0 + (k + kMovePieces) * rows;
-                src[k] = i < n ? kept[i] : 0;
+                for (int k = 0; k < C::kPieces; ++k)
+                    if (mine + c * step + k * kRows < n)
+                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;"
+                                     ::"r"(smem_u32(ring + ((c % kMoveStages) * C::kPieces + k) * C::kThreads + tid)), "l"(row(blk[k], src[k])) : "memory");
             }
-            __syncthreads();
+            asm volatile("cp.async.commit_group;" ::: "memory");
+        };
+        list(0);
+        for (int c = 0; c < kMoveStages - 1; ++c) {
+            load(c);
+            list(c + 1);
+        }
+        for (int c = 0; c < chunks; ++c) {
+            load(c + kMoveStages - 1);
+            list(c + kMoveStages);
+            asm volatile("cp.async.wait_group %0;" ::"n"(kMoveStages - 1) : "memory");  // this thread's rows of chunk c have been read
+            if constexpr (kCluster) {
+                // (It orders no stores: a barrier that releases would wait for those of the chunk before, 6 us a chunk.
+                // The reads that matter have returned.)
+                asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+                asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+            } else {
+                __syncthreads();
+            }
+            int blk[C::kPieces];
 #pragma unroll
-            for (int k = 0; k < kMovePieces; ++k)
-                if (i0 + r0 + k * rows < n) *reinterpret_cast<uint4*>(row(i0 + r0 + k * rows)) = x[k];
-            __syncthreads();
+            for (int k = 0; k < C::kPieces; ++k) blk[k] = table[min(mine + c * step + k * kRows, n - 1) / kPage];
+#pragma unroll
+            for (int k = 0; k < C::kPieces; ++k) {
+                const int i = mine + c * step + k * kRows;
+                if (i < n)
+                    *reinterpret_cast<uint4*>(row(blk[k], i)) = ring[((c % kMoveStages) * C::kPieces + k) * C::kThreads + tid];
+            }
         }
     }
     // the CTA that comes last shortens the requests: nobody reads their lengths any more
@@ -309,22 +379,12 @@ evict_move_kernel(const __grid_constant__ EvictParams p)
     }
 }
 
-cudaError_t launch_evict(const EvictParams& args, int head_dim, int num_sms, cudaStream_t st, bool pdl)
+template <typename... KArgs, typename... Args>
+static cudaError_t launch_clusters(void (*kernel)(KArgs...), dim3 grid, int threads, size_t smem, int nc, cudaStream_t st, bool pdl, Args... args)
 {
-    EvictParams p = args;
-    const long long units = (long long)p.num_slices * p.batch * p.num_kv_heads;
-    const long long max_pos = (long long)p.max_blocks_per_seq * kPage;
-    // as many CTAs per unit as give every SM two, or as its positions need to fit shared memory
-    int nc = 1;
-    while (nc < 8 && (units * nc < 2 * num_sms || max_pos > (long long)kSelCap * nc) && max_pos > 1024 * nc) nc *= 2;
-    p.part_cap = (int)((max_pos + nc - 1) / nc + 31) / 32 * 32;
-    if (p.part_cap > kSelCap) p.part_cap = kSelCap;
-    const int smem = p.part_cap * (int)sizeof(float);
-    cudaError_t e = cudaFuncSetAttribute(evict_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSelCap * (int)sizeof(float));
-    if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(units * nc));
-    cfg.blockDim = dim3(kSelThreads);
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
@@ -335,21 +395,38 @@ cudaError_t launch_evict(const EvictParams& args, int head_dim, int num_sms, cud
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = pdl ? 2 : 1;
-    e = cudaLaunchKernelEx(&cfg, evict_select_kernel, p, nc);
+    return cudaLaunchKernelEx(&cfg, kernel, KArgs(args)...);
+}
+
+template <int kRowPieces, bool kCluster>
+static cudaError_t launch_move(const EvictParams& p, dim3 grid, int nc, cudaStream_t st, bool pdl)
+{
+    using C = MoveCfg<kCluster>;
+    cudaError_t e = cudaFuncSetAttribute(evict_move_kernel<kRowPieces, kCluster>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem);
     if (e != cudaSuccess) return e;
-    // whole rows of K and of V where that fills the SMs, else narrower slices (not below 32 bytes: a DRAM sector)
-    int pieces = head_dim / 8, slices = 1;
-    while (pieces > 2 && units * 2 * slices < 3 * num_sms) {
-        pieces /= 2;
-        slices *= 2;
-    }
-    const dim3 grid((unsigned)units, 2 * slices), block(units * 2 * slices < 3 * num_sms ? 1024 : 256);
-    switch (pieces) {
-        case 16: return launch_ex(evict_move_kernel<16>, grid, block, 0, st, pdl, p);
-        case 8: return launch_ex(evict_move_kernel<8>, grid, block, 0, st, pdl, p);
-        case 4: return launch_ex(evict_move_kernel<4>, grid, block, 0, st, pdl, p);
-        default: return launch_ex(evict_move_kernel<2>, grid, block, 0, st, pdl, p);
-    }
+    return launch_clusters(evict_move_kernel<kRowPieces, kCluster>, grid, C::kThreads, C::kSmem, nc, st, pdl, p, nc);
+}
+
+cudaError_t launch_evict(const EvictParams& args, int head_dim, int num_sms, cudaStream_t st, bool pdl)
+{
+    EvictParams p = args;
+    const long long units = (long long)p.num_slices * p.batch * p.num_kv_heads;
+    const long long max_pos = (long long)p.max_blocks_per_seq * kPage;
+    // as many CTAs per unit as give every SM two, or as its positions need to fit shared memory
+    int nc = 1;
+    while (nc < 8 && (units * nc < 2 * num_sms || max_pos > (long long)kSelCap * nc) && max_pos > 1024 * nc) nc *= 2;
+    p.part_cap = (int)((max_pos + nc - 1) / nc + 31) / 32 * 32;
+    if (p.part_cap > kSelMost) p.part_cap = kSelMost;
+    cudaError_t e = cudaFuncSetAttribute(evict_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSelMost * (int)sizeof(float));
+    if (e != cudaSuccess) return e;
+    e = launch_clusters(evict_select_kernel, dim3((unsigned)(units * nc)), kSelThreads, p.part_cap * sizeof(float), nc, st, pdl, p, nc);
+    if (e != cudaSuccess) return e;
+    int mc = 1;
+    while (mc < 8 && units * 2 * mc < 3 * num_sms) mc *= 2;
+    const dim3 grid((unsigned)(units * mc), 2);
+    if (head_dim == 128)
+        return mc == 1 ? launch_move<16, false>(p, grid, 1, st, pdl) : launch_move<16, true>(p, grid, mc, st, pdl);
+    return mc == 1 ? launch_move<8, false>(p, grid, 1, st, pdl) : launch_move<8, true>(p, grid, mc, st, pdl);
 }
 
 }  // namespace oda
