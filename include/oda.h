@@ -400,7 +400,7 @@ oda_status_t oda_full_decode_weighted(oda_ctx_t* ctx, int32_t layer_begin, int32
  *   kept (nullable): [slices][batch][kv_heads][budget] i32, the old position of every new one; a request within the
  *     budget gets 0 .. t-1 and then -1, a masked one is not written.  Without it the list needs scratch (device,
  *     256-byte aligned, oda_evict_scratch_bytes(ctx) suffices for every budget); with it scratch may be NULL.
- *   weights: as in oda_full_decode_weighted.  All slices of the cache are treated, those of fixed-window layers too:
+ *   weights: as in oda_full_decode_weighted, 16-byte aligned (a kept -0 may become 0, a NaN another NaN).  All slices of the cache are treated, those of fixed-window layers too:
  *     choose `recent` at least as large as the largest window, and what a Local pass reads stays what it was.
  * The rows move inside the request's own pages: no other request may use a page of a request that is shortened
  * (a shared prefix is copied before its first eviction).  Pages behind the budget are free afterwards; the block table

@@ -22,20 +22,18 @@
 
 namespace oda {
 
-constexpr int kSelThreads = 512;
-constexpr int kSelWarps = kSelThreads / 32;
 constexpr int kSelCap = 24576;        // positions a CTA is meant to hold (96 KiB: two CTAs per SM)
 constexpr int kSelMost = 47104;       // and at most (184 KiB; longer parts are worked through in rounds)
-constexpr int kCopies = 8;            // of a CTA's histogram: lanes that count the same digit (most weights share a few
+constexpr int kCopies = 4;            // of a CTA's histogram: lanes that count the same digit (most weights share a few
                                       // exponents) rarely meet in one word
 
-// larger weight -> larger key; -0 and +0 are one key, NaN is above everything
-__device__ __forceinline__ uint32_t weight_key(float w)
+// Weights are held as their bits with -0 as 0 and every NaN as the largest positive pattern, so that the key is two
+// instructions: larger weight, larger key; -0 and 0 are one, NaN is above everything.
+__device__ __forceinline__ uint32_t weight_bits(float w)
 {
-    const uint32_t u = __float_as_uint(w + 0.f);  // -0 + 0 = +0
-    if (w != w) return 0xffffffffu;
-    return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
+    return w != w ? 0x7fffffffu : __float_as_uint(w + 0.f);
 }
+__device__ __forceinline__ uint32_t weight_key(uint32_t u) { return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u); }
 
 __device__ __forceinline__ uint32_t cluster_rank()
 {
@@ -61,6 +59,7 @@ __device__ __forceinline__ uint32_t cluster_peek(const uint32_t* var, uint32_t r
     return v;
 }
 
+template <int kSelWarps>
 struct SelShared {
     uint32_t hist[kCopies][256 + 4];
     uint32_t sum[3][256];             // this CTA's digits, a buffer per pass in turn: one is written, one may still be
@@ -68,16 +67,18 @@ struct SelShared {
     uint32_t total[256];              // the cluster's
     uint32_t counts[2][2];            // by parity of the round: positions heavier than T, and of weight T
     uint32_t wcount[kSelWarps];       // per warp: heavier | equal << 16
-    uint32_t prefix, left;
+    uint32_t prefix, left, zeros;     // zeros: weights of 0 among this CTA's candidates
 };
 
-__global__ void __launch_bounds__(kSelThreads)
+template <int kSelThreads>
+__global__ void __launch_bounds__(kSelThreads, kSelThreads == 512 ? 3 : 1)
 evict_select_kernel(const __grid_constant__ EvictParams p, const int nc)
 {
     griddep_wait();
     griddep_launch_dependents();
-    extern __shared__ float part[];   // this CTA's positions of the round
-    __shared__ SelShared sh;
+    extern __shared__ __align__(16) uint32_t part[];  // this CTA's positions of the round: weight_bits
+    constexpr int kSelWarps = kSelThreads / 32;
+    __shared__ SelShared<kSelWarps> sh;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int rank = nc > 1 ? (int)cluster_rank() : 0;
     const int unit = blockIdx.x / nc;
@@ -107,18 +108,20 @@ evict_select_kernel(const __grid_constant__ EvictParams p, const int nc)
     auto load_part = [&](int r) {
         const long long i0 = ((long long)r * nc + rank) * per;
         const int m = (int)max(0ll, min((long long)per, t - i0));
-        for (int i = tid; i < m; i += 4 * kSelThreads) {
-            float v[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) v[k] = i + k * kSelThreads < m ? __ldcg(w + i0 + i + k * kSelThreads) : 0.f;
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-                if (i + k * kSelThreads < m) part[i + k * kSelThreads] = v[k];
+        const float4* from = reinterpret_cast<const float4*>(w + i0);  // (i0 is a multiple of 32)
+        uint4* to = reinterpret_cast<uint4*>(part);
+        for (int i = tid; i < m / 4; i += 2 * kSelThreads) {
+            const bool two = i + kSelThreads < m / 4;
+            const float4 x = __ldcg(from + i), y = two ? __ldcg(from + i + kSelThreads) : x;
+            to[i] = make_uint4(weight_bits(x.x), weight_bits(x.y), weight_bits(x.z), weight_bits(x.w));
+            if (two) to[i + kSelThreads] = make_uint4(weight_bits(y.x), weight_bits(y.y), weight_bits(y.z), weight_bits(y.w));
         }
+        if (tid < m % 4) part[m / 4 * 4 + tid] = weight_bits(__ldcg(w + i0 + m / 4 * 4 + tid));
         return m;
     };
     if (tid < 256)
         for (int k = 0; k < kCopies; ++k) sh.hist[k][tid] = 0;
+    if (tid == 0) sh.zeros = 0;
     int m = 0;
     if (rounds == 1) m = load_part(0);
     __syncthreads();
@@ -129,21 +132,36 @@ evict_select_kernel(const __grid_constant__ EvictParams p, const int nc)
             const int shift = 24 - 8 * pass;
             const uint32_t above = pass == 0 ? 0u : 0xffffffffu << (shift + 8);
             uint32_t* hist = sh.hist[lane % kCopies];
-            // weights of 0 (positions nobody looked at) are one key and may be most of them: a warp adds them at once
-            auto count = [&](float v, bool there) {
-                const uint32_t k = weight_key(v);
-                const bool in = there && (k & above) == prefix;
-                const uint32_t zeros = __ballot_sync(0xffffffffu, in && v == 0.f);
-                if (in && v != 0.f) atomicAdd(&hist[(k >> shift) & 255u], 1u);
-                if (zeros && lane == 0) atomicAdd(&hist[(0x80000000u >> shift) & 255u], (uint32_t)__popc(zeros));
+            // (weights of 0 -- positions nobody looked at -- are one key and may be most of them: they are counted apart,
+            // in the first pass)
+            uint32_t zeros = 0;
+            auto count = [&](uint32_t u) {
+                const uint32_t k = weight_key(u);
+                if (u == 0)
+                    ++zeros;
+                else if ((k & above) == prefix)
+                    atomicAdd(&hist[(k >> shift) & 255u], 1u);
             };
             if (rounds == 1) {
                 const int i0 = rank * per;
                 const int from = max(0, lo - i0), to = min(m, hi - i0);
-                for (int i = from + warp * 32; i < to; i += kSelThreads) count(i + lane < to ? part[i + lane] : 0.f, i + lane < to);
+                for (int i = from / 4 * 4 + tid * 4; i < to; i += kSelThreads * 4) {
+                    const uint4 u = *reinterpret_cast<const uint4*>(part + i);
+                    if (i >= from && i + 4 <= to) {
+                        count(u.x); count(u.y); count(u.z); count(u.w);
+                    } else {
+                        if (i >= from) count(u.x);
+                        if (i + 1 >= from && i + 1 < to) count(u.y);
+                        if (i + 2 >= from && i + 2 < to) count(u.z);
+                        if (i + 3 >= from && i + 3 < to) count(u.w);
+                    }
+                }
             } else {
-                for (int i = lo + (rank * kSelWarps + warp) * 32; i < hi; i += nc * kSelThreads)
-                    count(i + lane < hi ? __ldcg(w + i + lane) : 0.f, i + lane < hi);
+                for (int i = lo + rank * kSelThreads + tid; i < hi; i += nc * kSelThreads) count(weight_bits(__ldcg(w + i)));
+            }
+            if (pass == 0) {
+                zeros = __reduce_add_sync(0xffffffffu, zeros);
+                if (lane == 0 && zeros) atomicAdd(&sh.zeros, zeros);
             }
             __syncthreads();
             if (tid < 256) {
@@ -153,6 +171,7 @@ evict_select_kernel(const __grid_constant__ EvictParams p, const int nc)
                     sum += sh.hist[k][tid];
                     sh.hist[k][tid] = 0;
                 }
+                if ((0x80000000u & above) == prefix && tid == (int)((0x80000000u >> shift) & 255u)) sum += sh.zeros;
                 (nc == 1 ? sh.total : sh.sum[pass % 3])[tid] = sum;
             }
             if (nc > 1) {
@@ -204,27 +223,37 @@ evict_select_kernel(const __grid_constant__ EvictParams p, const int nc)
             __syncthreads();
         }
         const long long i0 = ((long long)r * nc + rank) * per;
-        const int run = per / 32 / kSelWarps * 32 + 32;            // positions of one warp
+        const int run = per / 128 / kSelWarps * 128 + 128;         // positions of one warp
         const int j0 = warp * run, j1 = min(m, j0 + run);
-        auto classes = [&](int j, uint32_t& gt, uint32_t& eq) {    // of positions j + lane
-            bool is_gt = false, is_eq = false;
-            if (j + lane < j1) {
-                const long long i = i0 + j + lane;
-                const uint32_t k = weight_key(part[j + lane]);
-                const bool fixed = i < lo || i >= hi;
-                is_gt = fixed || (any && k > T);
-                is_eq = !fixed && any && k == T;
+        // of the four positions from j on: bits 0-3 heavier than T (or kept in any case), bits 4-7 of weight T
+        auto classes = [&](int j, const uint4& u) {
+            const uint32_t k[4] = {weight_key(u.x), weight_key(u.y), weight_key(u.z), weight_key(u.w)};
+            uint32_t c = 0;
+            if (any) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) c |= (k[e] > T ? 1u << e : 0u) | (k[e] == T ? 16u << e : 0u);
             }
-            gt = __ballot_sync(0xffffffffu, is_gt);
-            eq = __ballot_sync(0xffffffffu, is_eq);
+            const long long i = i0 + j;
+            if (i < lo || i + 4 > hi) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (i + e < lo || i + e >= hi) c = (c & ~(16u << e)) | (1u << e);
+            }
+            if (j + 4 > j1) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (j + e >= j1) c &= ~(17u << e);
+            }
+            return c;
         };
         uint32_t ngt = 0, neq = 0;
-        for (int j = j0; j < j1; j += 32) {
-            uint32_t gt, eq;
-            classes(j, gt, eq);
-            ngt += __popc(gt);
-            neq += __popc(eq);
+        for (int j = j0 + lane * 4; j < j1; j += 128) {
+            const uint32_t c = classes(j, *reinterpret_cast<const uint4*>(part + j));
+            ngt += __popc(c & 15u);
+            neq += __popc(c >> 4);
         }
+        ngt = __reduce_add_sync(0xffffffffu, ngt);
+        neq = __reduce_add_sync(0xffffffffu, neq);
         if (lane == 0) sh.wcount[warp] = ngt | (neq << 16);        // (at most 24,576 of each)
         __syncthreads();
         uint32_t gts = base_gt, eqs = base_eq, all_gt = 0, all_eq = 0;
@@ -256,24 +285,44 @@ evict_select_kernel(const __grid_constant__ EvictParams p, const int nc)
             base_eq += all_eq;
         }
         bool dropped = false;
-        for (int j = j0; j < j1; j += 32) {
-            uint32_t gt, eq;
-            classes(j, gt, eq);
-            const uint32_t below = (1u << lane) - 1u;
-            const uint32_t my_gt = gts + __popc(gt & below), my_eq = eqs + __popc(eq & below);
-            const bool keep = ((gt >> lane) & 1u) || (((eq >> lane) & 1u) && my_eq < left);
-            if (keep) {
-                const uint32_t dst = my_gt + min(my_eq, left);
-                kept[dst] = (int32_t)(i0 + j + lane);
-                w[dst] = part[j + lane];   // dst is not behind its source, and every weight of the round has been read
+        for (int jw = j0; jw < j1; jw += 128) {
+            const int j = jw + lane * 4;
+            uint4 u = make_uint4(0, 0, 0, 0);
+            uint32_t c = 0;
+            if (j < j1) {
+                u = *reinterpret_cast<const uint4*>(part + j);
+                c = classes(j, u);
             }
-            const uint32_t gone = __ballot_sync(0xffffffffu, !keep && j + lane < j1);
-            if (gone && !dropped) {
-                dropped = true;
-                if (lane == 0) atomicMin(first, (int)(i0 + j + __ffs(gone) - 1));
+            const uint32_t own = __popc(c & 15u) | (__popc(c >> 4) << 16);
+            uint32_t x = own;
+            for (int o = 1; o < 32; o <<= 1) {
+                const uint32_t y = __shfl_up_sync(0xffffffffu, x, o);
+                if (lane >= o) x += y;
             }
-            gts += __popc(gt);
-            eqs += __popc(eq);
+            uint32_t my_gt = gts + ((x - own) & 0xffffu), my_eq = eqs + ((x - own) >> 16);
+            const uint32_t bits[4] = {u.x, u.y, u.z, u.w};
+            int gone = 0x7fffffff;         // first of the four that is dropped
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const bool gt = (c >> e) & 1u, eq = (c >> (4 + e)) & 1u;
+                if (gt || (eq && my_eq < left)) {
+                    const uint32_t dst = my_gt + min(my_eq, left);
+                    kept[dst] = (int32_t)(i0 + j + e);
+                    w[dst] = __uint_as_float(bits[e]);  // dst is not behind its source, and every weight of the round has been read
+                } else if (j + e < j1 && gone == 0x7fffffff) {
+                    gone = (int)(i0 + j + e);
+                }
+                my_gt += gt;
+                my_eq += eq;
+            }
+            if (!dropped) {
+                gone = __reduce_min_sync(0xffffffffu, gone);
+                dropped = gone != 0x7fffffff;
+                if (dropped && lane == 0) atomicMin(first, gone);
+            }
+            const uint32_t sum = __shfl_sync(0xffffffffu, x, 31);
+            gts += sum & 0xffffu;
+            eqs += sum >> 16;
         }
         __syncthreads();                   // part and wcount are used again
     }
@@ -288,13 +337,14 @@ constexpr int kMoveStages = 3;
 template <bool kCluster>
 struct MoveCfg {
     static constexpr int kThreads = kCluster ? 512 : 256;
-    static constexpr int kPieces = kCluster ? 8 : 4;      // a thread's in one chunk
+    static constexpr int kPieces = 4;                     // a thread's in one chunk (96 KiB in all: two CTAs of a cluster may share
+                                                          // an SM, or the last clusters find no room beside the first)
     static constexpr int kStageBytes = kThreads * kPieces * 16;
     static constexpr int kSmem = kMoveStages * kStageBytes;
 };
 
 template <int kRowPieces, bool kCluster>
-__global__ void __launch_bounds__(MoveCfg<kCluster>::kThreads, kCluster ? 1 : 4)
+__global__ void __launch_bounds__(MoveCfg<kCluster>::kThreads, kCluster ? 2 : 4)
 evict_move_kernel(const __grid_constant__ EvictParams p, const int nc)
 {
     griddep_wait();
@@ -339,6 +389,10 @@ evict_move_kernel(const __grid_constant__ EvictParams p, const int nc)
             }
             asm volatile("cp.async.commit_group;" ::: "memory");
         };
+        // The CTAs' threads need not keep step at every chunk: a chunk may be stored once every row whose source lies before
+        // its end has been read.  `limit` is the source of the first row not known to have been read by all, and only
+        // where that lies inside the chunk do they meet: at a quarter kept, at chunks 0, 4, 20, 84, ...
+        int limit = kept[first];
         list(0);
         for (int c = 0; c < kMoveStages - 1; ++c) {
             load(c);
@@ -348,13 +402,16 @@ evict_move_kernel(const __grid_constant__ EvictParams p, const int nc)
             load(c + kMoveStages - 1);
             list(c + kMoveStages);
             asm volatile("cp.async.wait_group %0;" ::"n"(kMoveStages - 1) : "memory");  // this thread's rows of chunk c have been read
-            if constexpr (kCluster) {
-                // (It orders no stores: a barrier that releases would wait for those of the chunk before, 6 us a chunk.
-                // The reads that matter have returned.)
-                asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
-                asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
-            } else {
-                __syncthreads();
+            if (limit < min(first + (c + 1) * step, n)) {
+                if constexpr (kCluster) {
+                    // (it orders no stores: a barrier that releases would wait for those under way; the reads that
+                    // matter have returned)
+                    asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+                    asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+                } else {
+                    __syncthreads();
+                }
+                limit = first + (c + 1) * step < n ? kept[first + (c + 1) * step] : 0x7fffffff;
             }
             int blk[C::kPieces];
 #pragma unroll
@@ -407,6 +464,14 @@ static cudaError_t launch_move(const EvictParams& p, dim3 grid, int nc, cudaStre
     return launch_clusters(evict_move_kernel<kRowPieces, kCluster>, grid, C::kThreads, C::kSmem, nc, st, pdl, p, nc);
 }
 
+template <int kThreads>
+static cudaError_t launch_select(const EvictParams& p, long long units, int nc, cudaStream_t st, bool pdl)
+{
+    cudaError_t e = cudaFuncSetAttribute(evict_select_kernel<kThreads>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSelMost * (int)sizeof(float));
+    if (e != cudaSuccess) return e;
+    return launch_clusters(evict_select_kernel<kThreads>, dim3((unsigned)(units * nc)), kThreads, p.part_cap * sizeof(float), nc, st, pdl, p, nc);
+}
+
 cudaError_t launch_evict(const EvictParams& args, int head_dim, int num_sms, cudaStream_t st, bool pdl)
 {
     EvictParams p = args;
@@ -417,9 +482,8 @@ cudaError_t launch_evict(const EvictParams& args, int head_dim, int num_sms, cud
     while (nc < 8 && (units * nc < 2 * num_sms || max_pos > (long long)kSelCap * nc) && max_pos > 1024 * nc) nc *= 2;
     p.part_cap = (int)((max_pos + nc - 1) / nc + 31) / 32 * 32;
     if (p.part_cap > kSelMost) p.part_cap = kSelMost;
-    cudaError_t e = cudaFuncSetAttribute(evict_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSelMost * (int)sizeof(float));
-    if (e != cudaSuccess) return e;
-    e = launch_clusters(evict_select_kernel, dim3((unsigned)(units * nc)), kSelThreads, p.part_cap * sizeof(float), nc, st, pdl, p, nc);
+    // (long parts: one CTA per SM, and more threads to work through them)
+    cudaError_t e = p.part_cap > kSelCap ? launch_select<1024>(p, units, nc, st, pdl) : launch_select<512>(p, units, nc, st, pdl);
     if (e != cudaSuccess) return e;
     int mc = 1;
     while (mc < 8 && units * 2 * mc < 3 * num_sms) mc *= 2;

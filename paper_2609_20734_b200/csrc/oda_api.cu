@@ -1194,7 +1194,8 @@ oda_status_t oda_evict(oda_ctx_t* c, int32_t batch, float* weights, void* k, voi
     if (!c->ws) return fail(c, ODA_ERR_WORKSPACE, "oda_set_workspace has not been called");
     if (batch == 0) return ODA_OK;
     if (!weights || !k || !v || !bt || !sl) return fail(c, ODA_ERR_INVALID_ARG, "null pointer");
-    if (!aligned16(k) || !aligned16(v)) return fail(c, ODA_ERR_INVALID_ARG, "the caches must be 16-byte aligned");
+    if (!aligned16(k) || !aligned16(v) || !aligned16(weights))
+        return fail(c, ODA_ERR_INVALID_ARG, "the caches and weights must be 16-byte aligned");
     if (!kept) {
         const size_t need = (size_t)c->phys_layers * batch * f.num_kv_heads * budget * sizeof(int32_t);
         if (!scratch || (reinterpret_cast<uintptr_t>(scratch) % kAlign) != 0 || scratch_bytes < need)
