@@ -23,10 +23,11 @@
 //
 // Two forms of the kernel, chosen by the most rows that a kv head can have in the call (batch x group):
 //   narrow (<= 128 rows): bound by the stream of K and V.  One copy of Q, and the rest of shared memory as a ring.
-//   wide: bound by the products and the exponentials.  2 x 128 rows, and S twice for each: while the softmax of a tile
-//     runs, the product for the next one has been made, so that neither waits for the other.  (With S once, the two
-//     streams fall into step -- both compute exponentials, then both wait for products -- and a pair of
-//     128-position tiles took 6,000 cycles.)
+//   wide: bound by the products and the exponentials.  2 x 128 rows.
+// S has two buffers a stream (where TMEM holds them): while the softmax of a tile runs, the product for the stream's
+// next one is made, so that neither waits for the other.  With one, two row tiles fell into step -- both computed
+// exponentials, then both waited for products: 6,000 cycles for 128 positions -- and the narrow form spent
+// 2,400 cycles on the chain from one tile of a stream to its next.
 //
 // P in bf16 is kTerms parts of 8 bits each.  fp32 results take three (24 bits: nothing is lost against fp32
 // arithmetic), bf16 results two in the narrow form, where the second product hides behind the stream.
@@ -56,7 +57,10 @@ struct ShCfg {
     static constexpr int kQBytes = kShRows * D * 2;
     static constexpr int kQTiles = kWide ? 2 : 1;
     static constexpr int kSpCols = kTokens / 2 * kTerms > kTokens ? kTokens / 2 * kTerms : kTokens;  // one S, then P
-    static constexpr int kBufs = kWide && 4 * kSpCols + 2 * D <= 512 ? 2 : 1;
+    static constexpr int kBufs = 4 * kSpCols + 2 * D <= 512 ? 2 : 1;
+    // tiles that K runs ahead of V: those whose S there is room for
+    static constexpr int kAhead = 2 * kBufs;                // streams in turn
+    static constexpr int kAheadDual = kBufs;                // both streams on every tile
     static constexpr int kO0 = 2 * kBufs * kSpCols;         // first column of stream 0's O
     static constexpr int kRowBlock = kWide ? 256 : 128;     // rows of a unit
     static_assert(kO0 + 2 * D <= 512, "TMEM");
@@ -354,7 +358,7 @@ shared_prefix_kernel(const __grid_constant__ SharedParams p, const __grid_consta
         for (int x = x0; x < x1 && !dead;) {
             const ShItem it = shared_item<TP, C::kRowBlock>(p, pl, x, x1);
             x += it.n;
-            const int ahead = kWide && it.nrows > kShRows ? C::kBufs : 2;
+            const int ahead = kWide && it.nrows > kShRows ? C::kAheadDual : C::kAhead;
             const int lead = pl.g.list[pl.g.gs[it.group]];
             const int32_t* table = p.block_table + (size_t)lead * p.max_blocks_per_seq;
             const int first = it.tile0 * TP, last = min(it.pages, (it.tile0 + it.n) * TP);
@@ -432,10 +436,10 @@ shared_prefix_kernel(const __grid_constant__ SharedParams p, const __grid_consta
             const int n = __shfl_sync(0xffffffffu, item.n, 0);
             const bool dual = kWide && __shfl_sync(0xffffffffu, item.nrows, 0) > kShRows;
             const int rest = __shfl_sync(0xffffffffu, item.pages - item.tile0 * TP, 0);  // pages from the item's first on
-            const int ahead = dual ? C::kBufs : 2, lead = min(ahead, n);
+            const int ahead = dual ? C::kAheadDual : C::kAhead, lead = min(ahead, n);
             const int step = dual ? 1 : 2, t0 = dual ? 0 : s;     // the stream's tiles: t0, t0 + step, ...
             const int nt = t0 < n ? (n - t0 + step - 1) / step : 0;
-            const int bufs = dual ? C::kBufs : 1;
+            constexpr int bufs = C::kBufs;
             // slots in the producers' order: K_0 .. K_(lead-1) alone, then V_t with K_(t+ahead)
             uint32_t slot = 0, phase = 0;
             auto go_to = [&](uint32_t at) { slot = at % C::kSlots; phase = (at / C::kSlots) & 1; };
@@ -550,7 +554,8 @@ shared_prefix_kernel(const __grid_constant__ SharedParams p, const __grid_consta
             }
             float m = -INFINITY, l = 0.f;  // m in log2 units
             bool fresh = true;
-            const int step = dual ? 1 : 2, t0 = dual ? 0 : s, bufs = dual ? C::kBufs : 1;
+            const int step = dual ? 1 : 2, t0 = dual ? 0 : s;
+            constexpr int bufs = C::kBufs;
             const int nt = (it.n - t0 + step - 1) / step;
             for (int i = 0; i < nt; ++i) {
                 const int t = t0 + i * step, u = bufs == 2 ? i & 1 : 0;
