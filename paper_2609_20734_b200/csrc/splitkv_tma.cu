@@ -158,11 +158,10 @@ struct PageRun {
 //                form from the one length.  The others do not carry that code.
 //  kInstScores   the weighted Full pass: it also writes its logits (fp32, group x 4 bytes a position
 //                beside 4 D bytes of K and V) and each row's (m, 1 / l) for the kernel that adds the
-//                weights up.  It keeps P as three bf16 parts: 24 bits, so that fp32 results are as good
-//                as fp32 arithmetic makes them (two parts leave 1.6e-6 of the result; the third product
-//                is hidden behind the stream).
+//                weights up.  For fp32 results it keeps P as three bf16 parts: 24 bits, as good as fp32
+//                arithmetic (two parts leave 1.6e-6 of the result).
 //  kInstTail     the tails of requests that share prefixes (shared_prefix.cu): it skips the shared pages and
-//                leaves each row as a partial result.  Three parts of P like kInstScores.  It runs beside the
+//                leaves each row as a partial result.  Parts of P like kInstScores.  It runs beside the
 //                kernel before it: that one lets its dependents start only once everything before IT has
 //                finished, so lengths, flags and caches are final, and nothing here reads what it writes.  Every
 //                CTA waits for it before it ends, so that what follows this kernel follows both.
@@ -685,7 +684,7 @@ splitkv_tma_kernel(const __grid_constant__ AttnParams p, const __grid_constant__
                     const uint32_t bh0 = movmatrix_t(hi0), bh1 = movmatrix_t(hi1);
                     const uint32_t bl0 = movmatrix_t(lo0), bl1 = movmatrix_t(lo1);
                     uint32_t bt0 = 0, bt1 = 0;  // third part of P
-                    if constexpr (kInst >= kInstScores) {
+                    if (kInst >= kInstScores && !p.out_bf16) {
                         const float r0 = p0 - __uint_as_float(hi0 << 16) - __uint_as_float(lo0 << 16);
                         const float r1 = p1 - __uint_as_float(hi0 & 0xffff0000u) - __uint_as_float(lo0 & 0xffff0000u);
                         const float r2 = p2 - __uint_as_float(hi1 << 16) - __uint_as_float(lo1 << 16);
@@ -705,7 +704,7 @@ splitkv_tma_kernel(const __grid_constant__ AttnParams p, const __grid_constant__
                         }
                         mma16816(o[mt], a0, a1, a2, a3, bh0, bh1);
                         mma16816(o[mt], a0, a1, a2, a3, bl0, bl1);
-                        if constexpr (kInst >= kInstScores) mma16816(o[mt], a0, a1, a2, a3, bt0, bt1);
+                        if (kInst >= kInstScores && !p.out_bf16) mma16816(o[mt], a0, a1, a2, a3, bt0, bt1);
                     }
                 }
                 __syncwarp();
