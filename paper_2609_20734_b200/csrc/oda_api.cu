@@ -229,14 +229,15 @@ oda_status_t launch_attention(oda_ctx* c, int mode, int lb, int le, int batch, c
     p.done_counter = reinterpret_cast<int32_t*>(c->ws + c->lay.status + 128);
     p.exit_counter = reinterpret_cast<int32_t*>(c->ws + c->lay.status + 192);
     p.num_sms = c->num_sms;
-    if (c->calibrating && !(extra && extra->shared))  // (tails wait for the other kernel: no rates to learn)
-        p.sm_stats = reinterpret_cast<unsigned long long*>(c->ws + c->lay.sm_bytes);
+    if (c->calibrating && !extra) p.sm_stats = reinterpret_cast<unsigned long long*>(c->ws + c->lay.sm_bytes);
     if (c->calibrated) {
         p.cum_share = reinterpret_cast<const uint16_t*>(c->ws + c->lay.cum_share);
         p.sm_claims = reinterpret_cast<int32_t*>(c->ws + c->lay.sm_claims);
     }
     if (advanced) *advanced = advance != nullptr;
     if (extra) {
+        p.claims = reinterpret_cast<int32_t*>(c->ws + c->lay.status + 40);  // (instead of the calibrated split)
+        p.cum_share = nullptr;
         p.score_rows = extra->score_rows;
         p.score_ml = extra->score_ml;
         if (const SharedParams* sp = extra->shared) {
@@ -417,7 +418,7 @@ oda_status_t oda_create(const oda_config_t* cfg, oda_ctx_t** out_ctx)
         c->num_sms = 148;  // no device visible: sizes follow a B200 so that host-only checks still work
         c->grid = 148 * 2;
     }
-    c->max_items = c->grid + cfg->num_layers * cfg->max_batch * cfg->num_kv_heads;
+    c->max_items = kClaimSpans * c->grid + cfg->num_layers * cfg->max_batch * cfg->num_kv_heads;
     c->head_grid = cfg->head_d_hidden > 0 ? recall_head_grid(cfg->head_d_hidden) : 1;
     compute_layout(c);
     *out_ctx = c;

@@ -79,6 +79,8 @@ struct AttnParams {
     int32_t num_groups;
     float* tail_o;              // [layers][batch][q heads][D], unnormalised
     float2* tail_ml;            // [layers][batch][q heads]: (m in log2 units, l)
+    // Score and tail instances: {spans claimed beyond the grid's first, CTAs that are done}, zero between launches
+    int32_t* claims;
 };
 
 // Programmatic dependent launch: a kernel launched with the stream-serialisation attribute may
@@ -111,6 +113,12 @@ __device__ __forceinline__ int32_t ld_meta_s32(const int32_t* ptr)
 // of the SM the CTA runs on:
 // the CTA reads %smid, claims one of that SM's two spans, and all CTAs finish together.
 constexpr int kMaxGrid = 320;
+
+// A launch with `claims` is cut into up to kClaimSpans spans per CTA, as long as each has kClaimMinPages pages: a CTA that
+// is done with its own takes the next that nobody has.  That evens out what the equal split leaves uneven without a
+// calibration run, at the price of more partials.  Which CTA streams a span does not change the bits.
+constexpr int kClaimSpans = 16;
+constexpr int kClaimMinPages = 96;
 
 struct Plan {  // shared memory, one per CTA
     int32_t pb[kMaxClasses][kMaxBatch + 1];  // exclusive prefix over requests of pages per kv head
@@ -339,6 +347,7 @@ __device__ inline void build_plan(const AttnParams& p, Plan& pl, const int32_t* 
             // (rounded down: a launch of 17 pages is one span, not two of eight and a half with a merge
             // between them, and units of 65 pages on spans of 16 are cut at their own boundaries)
             if (carry < (long long)g * minS) n = carry > 0 ? max(1ll, carry / minS) : 0;
+            if (p.claims && carry >= 2ll * g * kClaimMinPages) n = g * min((long long)kClaimSpans, carry / ((long long)g * kClaimMinPages));
             nseg = (int)n;
             pl.nseg = nseg;
             // the weighted split needs every CTA to have real work; small launches stay equal

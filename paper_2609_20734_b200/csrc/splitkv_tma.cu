@@ -173,6 +173,7 @@ splitkv_tma_kernel(const __grid_constant__ AttnParams p, const __grid_constant__
 {
     using C = TmaCfg<D>;
     constexpr bool kUniform = kInst == kInstUniform;
+    constexpr bool kClaims = kInst >= kInstScores;  // may stream more than one span
     extern __shared__ __align__(1024) uint8_t smem[];
     uint8_t* ring = smem;                                                 // kStages * kStageBytes
     uint8_t* qring = ring + C::kStages * C::kStageBytes;                  // kStages * kQSlotBytes
@@ -284,6 +285,12 @@ splitkv_tma_kernel(const __grid_constant__ AttnParams p, const __grid_constant__
         }
         int v = 0, nv = item_pages(it);  // next page of the item in streaming order, pages it has
         bool more = true, item_first = true;
+        // the next span to stream once this one is done, asked for ahead of time (the answer is lane 0's)
+        int claimed = 0x7fffffff;
+        const bool claiming = kClaims && p.claims && plan.nseg > (int)gridDim.x;
+        auto claim = [&]() {
+            if (claiming && lane == 0) claimed = (int)gridDim.x + atomicAdd(p.claims, 1);
+        };
         auto fetch = [&](PageRun& r, int& blk) -> bool {  // next run and its block ids; false when the span is done
             if (!more) return false;
             r.g = it.g; r.kv_layer = it.kv_layer; r.b = it.b; r.layer = it.layer;
@@ -306,12 +313,25 @@ splitkv_tma_kernel(const __grid_constant__ AttnParams p, const __grid_constant__
                     item_first = true;
                 } else {
                     more = false;
+                    if constexpr (kClaims) {
+                        const int j = claiming ? __shfl_sync(0xffffffffu, claimed, 0) : 0x7fffffff;
+                        if (j < plan.nseg) {
+                            claim();
+                            span_range(plan, j, x, x_end);
+                            take = decode_item(p, plan, j, x, x_end, it);
+                            span = j;
+                            v = 0;
+                            nv = item_pages(it);
+                            item_first = more = true;
+                        }
+                    }
                 }
             }
             return true;
         };
         PageRun cur, nxt;
         int blk_cur = 0, blk_nxt = 0;
+        if constexpr (kClaims) claim();
         bool have = fetch(cur, blk_cur);
         while (have && !dead) {
             // the next run is decoded, and its block ids requested, once this run's first tile is on
@@ -357,6 +377,16 @@ splitkv_tma_kernel(const __grid_constant__ AttnParams p, const __grid_constant__
             const uint32_t c2 = cnt - 1 - k;
             const uint32_t s = c2 % C::kStages, ph = (c2 / C::kStages) & 1;
             if (!mbar_wait(empty0 + 8 * s, ph, abort_flag, p.status)) break;
+        }
+        if constexpr (kClaims) {
+            if (!dead && lane == 0) {   // a stage with nothing in it: no more items
+                ctl.item_take[cnt % C::kStages] = 0;
+                mbar_arrive(full0 + 8 * (cnt % C::kStages));
+            }
+            if (claiming && lane == 0) {
+                __threadfence();
+                if (atomicAdd(p.claims + 1, 1) == (int)gridDim.x - 1) p.claims[0] = p.claims[1] = 0;
+            }
         }
         if (*abort_flag) {  // abandoned waits: give in-flight copies time to land before the CTA retires
             for (int i = 0; i < 1000; ++i) __nanosleep(1000);
@@ -583,13 +613,14 @@ splitkv_tma_kernel(const __grid_constant__ AttnParams p, const __grid_constant__
         if (kUniform && dp.ok == 2) uniform_span(dp, span, x, x_end);
         else if (!dp.ok) span_range(plan, span, x, x_end);
         span_pages = x_end - x;
-        while (x < x_end && !aborted) {
+        while ((kClaims || x < x_end) && !aborted) {
             Item it;
             // the item's descriptor and its Q^T fragments come with the item's first tile; heads >= G stay zero
             uint32_t qa[D / 16][2];
             {
                 const uint32_t s = cnt % C::kStages, ph = (cnt / C::kStages) & 1;
                 if (!mbar_wait(full0 + 8 * s, ph, abort_flag, p.status)) { aborted = true; break; }
+                if (kClaims && ctl.item_take[s] == 0) break;  // no more items
                 it = ctl.items[s];
                 x += ctl.item_take[s];
                 if (cnt == 0 && p.sm_stats) t_first = globaltimer_ns();
