@@ -1243,12 +1243,14 @@ static SharedScratch shared_scratch(const oda_ctx* c)
     size_t off = 0;
     auto take = [&](size_t bytes) { size_t o = off; off = align_up(off + bytes); return o; };
     w.desc = take(sizeof(SharedDesc));
-    w.ext_row0 = (size_t)f.num_layers * f.max_batch * f.num_q_heads;
+    const size_t tails = (size_t)f.num_layers * f.max_batch * f.num_q_heads;
+    // one partial of every row, or up to four where a kv head has no more than 128 of them
+    w.ext_row0 = std::max(tails, 4 * (size_t)f.num_layers * f.num_kv_heads * std::min(128, f.max_batch * c->group));
     const size_t rows = w.ext_row0 + (size_t)c->num_sms * 256;  // and the rows of one block for every span
     w.ml = take(rows * sizeof(float2));
     w.o = take(rows * f.head_dim * sizeof(float));
-    w.tail_ml = take(w.ext_row0 * sizeof(float2));
-    w.tail_o = take(w.ext_row0 * f.head_dim * sizeof(float));
+    w.tail_ml = take(tails * sizeof(float2));
+    w.tail_o = take(tails * f.head_dim * sizeof(float));
     w.total = off;
     return w;
 }

@@ -34,6 +34,7 @@
 #include <cuda.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "launch_ex.cuh"
 #include "mbar.cuh"
@@ -82,6 +83,11 @@ struct ShCtl {
     int32_t abort;
     float2 ml1[kShRows];             // stream 1's (m, l) when the streams are joined
 };
+
+// Few rows leave most of a 128-row tile, and most of the softmax warps, idle.  The tile then holds every row 2 or 4 times
+// (at 64 or 32 rows), and each copy's warps take a half or a quarter of a tile's columns: P is zero elsewhere, and the
+// copies are partial results of their own.
+__device__ __forceinline__ int row_copies(int nrows) { return nrows <= 32 ? 4 : nrows <= 64 ? 2 : 1; }
 
 struct ShItem {
     int32_t gl, kvh, group, row0, nrows, tile0, n, pages;  // gated layer index, ..., first row, rows, first tile, tiles, pages of the prefix
@@ -151,6 +157,21 @@ __device__ __forceinline__ void tc_st16(uint32_t addr, const uint32_t* r)
         ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
           "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
         : "memory");
+}
+__device__ __forceinline__ void tc_ld16(uint32_t addr, float* v)
+{
+    uint32_t* r = reinterpret_cast<uint32_t*>(v);
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(addr));
+}
+__device__ __forceinline__ void tc_st8(uint32_t addr, const uint32_t* r)
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+                 ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+                 : "memory");
 }
 // Shared-memory operand, 128-byte swizzle.  K-major (Q, K): rows of 128 bytes, groups of 8 rows 1024 bytes apart (lbo
 // not used).  MN-major (V): 64 columns of a position are one 128-byte row, groups of 8 positions 1024 bytes apart, the
@@ -255,7 +276,8 @@ __device__ __forceinline__ void shared_plan(const SharedParams& p, ShPlan& pl)
         for (int l = tid; l < p.num_gated; l += blockDim.x) d.gated_index[p.layer[l]] = l;
         if (tid < B) {
             SharedRow r;
-            r.unit = r.tiles = r.row = r.pad = 0;
+            r.unit = r.tiles = r.row = 0;
+            r.copies = 1;
             const int i = shared_group_of(g, NG, tid);
             if (i >= 0 && pl.total > 0) {
                 int rank = 0;
@@ -264,6 +286,7 @@ __device__ __forceinline__ void shared_plan(const SharedParams& p, ShPlan& pl)
                 r.tiles = (g.pages[i] + TP - 1) / TP;
                 r.unit = pl.off[i] + block * r.tiles;
                 r.row = (rank - block * per) * p.group;
+                if (kRowBlock == kShRows) r.copies = row_copies(g.members[i] * p.group);  // (the narrow form)
             }
             d.rows[tid] = r;
         }
@@ -520,14 +543,110 @@ shared_prefix_kernel(const __grid_constant__ SharedParams p, const __grid_consta
         const uint32_t sp0 = tmem + ((uint32_t)(warp & 3) << 21) + s * C::kBufs * C::kSpCols;
         const uint32_t oc = tmem + ((uint32_t)(warp & 3) << 21) + C::kO0;
         const float scale = p.scale_log2e;
+        const size_t own_rows = (size_t)p.num_gated * p.batch * p.num_q_heads;
         uint32_t ns[2] = {0, 0}, nd[2] = {0, 0}, nj = 0;  // tiles seen in each buffer, items that ended in it
         bool ok = true;
+        float m = -INFINITY, l = 0.f;  // of the item; m in log2 units
+        // tile i of nt: S in buffer u becomes P (columns of this copy only), m and l go on
+        auto softmax_tile = [&](auto copies_c, uint32_t sp, int i, int u, int nt, int cols, int copy) -> bool {
+            constexpr int kCopies = decltype(copies_c)::value, kCols = TN / kCopies;
+            constexpr int kRun = kCols < 32 ? kCols : 32;
+            const int c_first = kCopies == 1 ? 0 : copy * kCols;
+            float v[kCols], mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+            auto read = [&](int c0) {
+                if constexpr (kRun == 32) tc_ld32(sp + c_first + c0, v + c0);
+                else tc_ld16(sp + c_first + c0, v + c0);
+            };
+            read(0);
+#pragma unroll
+            for (int c0 = 0; c0 < kCols; c0 += kRun) {  // the next columns are on their way while these are looked at
+                tc_wait_ld();
+                if (c0 + kRun < kCols) read(c0 + kRun);
+                if (cols < c_first + c0 + kRun) {
+#pragma unroll
+                    for (int c = c0; c < c0 + kRun; ++c) v[c] = c_first + c < cols ? v[c] : -INFINITY;
+                }
+#pragma unroll
+                for (int c = c0; c < c0 + kRun; ++c) mx[c & 3] = fmaxf(mx[c & 3], v[c]);
+            }
+            const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * scale;
+            // The running maximum only moves when it would grow by more than 2^8: any value near the true one gives the
+            // same quotient, and O in TMEM then rarely has to be scaled.
+            if (i == 0) {
+                m = top;
+            } else if (__any_sync(0xffffffffu, top > m + 8.f)) {
+                // O has to be at rest.  This buffer's last product is complete (S was made behind it); the other buffer's
+                // is once its next S is, or at the end once it says so itself.
+                if (C::kBufs == 2) {
+                    const uint64_t* bar = i + 1 < nt ? &ctl.s_full[s][u ^ 1] : &ctl.pv_done[s][u ^ 1];
+                    const uint32_t at = i + 1 < nt ? (u ? ns[0] : ns[1]) : (u ? nd[0] : nd[1]);
+                    if (!warp_wait(bar, at & 1, abort_flag, p.status)) return false;
+                    tc_fence_after();
+                }
+                const float mn = top > m + 8.f ? top : m;
+                const float a = m == -INFINITY ? 0.f : ex2(m - mn);
+                m = mn;
+                l *= a;
+#pragma unroll
+                for (int c = 0; c < D; c += 32) {
+                    float o[32];
+                    tc_ld32(oc + s * D + c, o);
+                    tc_wait_ld();
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) o[e] *= a;
+                    tc_st32(oc + s * D + c, o);
+                }
+            }
+            const float mu = m == -INFINITY ? 0.f : m;
+            const uint64_t scale2 = pair(scale, scale), mu2 = pair(-mu, -mu);
+            uint64_t sum[2] = {0ull, 0ull};
+#pragma unroll
+            for (int c0 = 0; c0 < kCols; c0 += kRun) {
+                uint32_t part[kTerms][kRun / 2];
+#pragma unroll
+                for (int e = 0; e < kRun; e += 2) {
+                    const float2 z = unpair(fma2(pair(v[c0 + e], v[c0 + e + 1]), scale2, mu2));
+                    uint64_t w = pair(ex2(z.x), ex2(z.y));
+                    sum[(e >> 1) & 1] = add2(sum[(e >> 1) & 1], w);
+#pragma unroll
+                    for (int k = 0; k < kTerms; ++k) {
+                        const float2 a = unpair(w);
+                        const uint32_t pk = pack2(a.x, a.y);
+                        part[k][e / 2] = pk;
+                        if (k + 1 < kTerms)  // what is left after this part (exact)
+                            w = add2(w, pair(-__uint_as_float(pk << 16), -__uint_as_float(pk & 0xffff0000u)));
+                    }
+                }
+#pragma unroll
+                for (int k = 0; k < kTerms; ++k) {
+                    if constexpr (kRun == 32) tc_st16(sp + k * (TN / 2) + (c_first + c0) / 2, part[k]);
+                    else tc_st8(sp + k * (TN / 2) + (c_first + c0) / 2, part[k]);
+                }
+            }
+            if constexpr (kCopies > 1) {  // the other copies' columns
+                const uint32_t none[16] = {};
+#pragma unroll
+                for (int k = 0; k < kTerms; ++k)
+#pragma unroll
+                    for (int q = 1; q < kCopies; ++q) {
+                        const int other = (copy + q) % kCopies;
+                        if constexpr (kCopies == 2) tc_st16(sp + k * (TN / 2) + other * (kCols / 2), none);
+                        else tc_st8(sp + k * (TN / 2) + other * (kCols / 2), none);
+                    }
+            }
+            const float2 sums = unpair(add2(sum[0], sum[1]));
+            l += sums.x + sums.y;
+            tc_wait_st();
+            return true;
+        };
         for (int x = x0; x < x1 && ok;) {
             const ShItem it = shared_item<TP, C::kRowBlock>(p, pl, x, x1);
             x += it.n;
             const bool dual = kWide && it.nrows > kShRows;
             if (!dual && s == 1 && it.n == 1) continue;  // a lone tile: stream 0's
-            const int row = dual ? s * kShRows + tr : tr;
+            const int copies = kWide ? 1 : row_copies(it.nrows), per_copy = kShRows / copies;
+            const int copy = kWide ? 0 : tr / per_copy;
+            const int row = dual ? s * kShRows + tr : kWide ? tr : tr % per_copy;
             const bool valid = row < it.nrows;
             const bool warp_valid = (row & ~31) < it.nrows;
             const int layer = p.layer[it.gl];
@@ -552,8 +671,8 @@ shared_prefix_kernel(const __grid_constant__ SharedParams p, const __grid_consta
                 __syncwarp();
                 if (lane == 0) mbar_arrive(smem_u32(&ctl.q_full[s]));
             }
-            float m = -INFINITY, l = 0.f;  // m in log2 units
-            bool fresh = true;
+            m = -INFINITY;
+            l = 0.f;
             const int step = dual ? 1 : 2, t0 = dual ? 0 : s;
             constexpr int bufs = C::kBufs;
             const int nt = (it.n - t0 + step - 1) / step;
@@ -565,74 +684,10 @@ shared_prefix_kernel(const __grid_constant__ SharedParams p, const __grid_consta
                 tc_fence_after();
                 if (warp_valid) {
                     const int cols = min(TP, it.pages - (it.tile0 + t) * TP) * kPage;
-                    float v[TN], mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-                    tc_ld32(sp, v);
-#pragma unroll
-                    for (int c0 = 0; c0 < TN; c0 += 32) {  // the next 32 columns are on their way while these are looked at
-                        tc_wait_ld();
-                        if (c0 + 32 < TN) tc_ld32(sp + c0 + 32, v + c0 + 32);
-                        if (cols < TN) {
-#pragma unroll
-                            for (int c = c0; c < c0 + 32; ++c) v[c] = c < cols ? v[c] : -INFINITY;
-                        }
-#pragma unroll
-                        for (int c = c0; c < c0 + 32; ++c) mx[c & 3] = fmaxf(mx[c & 3], v[c]);
-                    }
-                    const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * scale;
-                    // The running maximum only moves when it would grow by more than 2^8: any value near the true one
-                    // gives the same quotient, and O in TMEM then rarely has to be scaled.
-                    if (fresh) {
-                        m = top;
-                        fresh = false;
-                    } else if (__any_sync(0xffffffffu, top > m + 8.f)) {
-                        // O has to be at rest.  This buffer's last product is complete (S was made behind it); the other
-                        // buffer's is once its next S is, or at the end once it says so itself.
-                        if (bufs == 2) {
-                            const uint64_t* bar = i + 1 < nt ? &ctl.s_full[s][u ^ 1] : &ctl.pv_done[s][u ^ 1];
-                            const uint32_t at = i + 1 < nt ? (u ? ns[0] : ns[1]) : (u ? nd[0] : nd[1]);
-                            if (!warp_wait(bar, at & 1, abort_flag, p.status)) { ok = false; break; }
-                            tc_fence_after();
-                        }
-                        const float mn = top > m + 8.f ? top : m;
-                        const float a = m == -INFINITY ? 0.f : ex2(m - mn);
-                        m = mn;
-                        l *= a;
-#pragma unroll
-                        for (int c = 0; c < D; c += 32) {
-                            float o[32];
-                            tc_ld32(oc + s * D + c, o);
-                            tc_wait_ld();
-#pragma unroll
-                            for (int e = 0; e < 32; ++e) o[e] *= a;
-                            tc_st32(oc + s * D + c, o);
-                        }
-                    }
-                    const float mu = m == -INFINITY ? 0.f : m;
-                    const uint64_t scale2 = pair(scale, scale), mu2 = pair(-mu, -mu);
-                    uint64_t sum[2] = {0ull, 0ull};
-#pragma unroll
-                    for (int c0 = 0; c0 < TN; c0 += 32) {
-                        uint32_t part[kTerms][16];
-#pragma unroll
-                        for (int e = 0; e < 32; e += 2) {
-                            const float2 z = unpair(fma2(pair(v[c0 + e], v[c0 + e + 1]), scale2, mu2));
-                            uint64_t w = pair(ex2(z.x), ex2(z.y));
-                            sum[(e >> 1) & 1] = add2(sum[(e >> 1) & 1], w);
-#pragma unroll
-                            for (int k = 0; k < kTerms; ++k) {
-                                const float2 a = unpair(w);
-                                const uint32_t pk = pack2(a.x, a.y);
-                                part[k][e / 2] = pk;
-                                if (k + 1 < kTerms)  // what is left after this part (exact)
-                                    w = add2(w, pair(-__uint_as_float(pk << 16), -__uint_as_float(pk & 0xffff0000u)));
-                            }
-                        }
-#pragma unroll
-                        for (int k = 0; k < kTerms; ++k) tc_st16(sp + k * (TN / 2) + c0 / 2, part[k]);
-                    }
-                    const float2 sums = unpair(add2(sum[0], sum[1]));
-                    l += sums.x + sums.y;
-                    tc_wait_st();
+                    if (copies == 1) ok = softmax_tile(std::integral_constant<int, 1>{}, sp, i, u, nt, cols, copy);
+                    else if (copies == 2) ok = softmax_tile(std::integral_constant<int, 2>{}, sp, i, u, nt, cols, copy);
+                    else ok = softmax_tile(std::integral_constant<int, 4>{}, sp, i, u, nt, cols, copy);
+                    if (!ok) break;
                 }
                 tc_fence_before();
                 __syncwarp();
@@ -664,8 +719,8 @@ shared_prefix_kernel(const __grid_constant__ SharedParams p, const __grid_consta
                 }
             }
             if (warp_valid && (dual || s == 0)) {
-                const size_t dst = it.tile0 == 0 ? ((size_t)it.gl * p.batch + b) * p.num_q_heads + head
-                                                 : p.ext_row0 + (size_t)span * 256 + row;
+                const size_t dst = it.tile0 == 0 ? copy * own_rows + ((size_t)it.gl * p.batch + b) * p.num_q_heads + head
+                                                 : p.ext_row0 + (size_t)span * 256 + (dual ? row : tr);
 #pragma unroll
                 for (int c = 0; c < D; c += 32) {
                     float o[32];
@@ -712,71 +767,103 @@ shared_prefix_kernel(const __grid_constant__ SharedParams p, const __grid_consta
     }
 }
 
-// One warp per row of a flagged request: tail and prefix chunks joined by log-sum-exp, rounded once.  Chunks are
-// taken eight at a time, all their loads before the first use.
-template <int V, bool kBf16>
+// kWarps warps per row of a flagged request: tail and prefix chunks joined by log-sum-exp, rounded once.  A warp takes its
+// chunks eight at a time, all their loads before the first use.  One warp is enough where rows are many; where they are
+// few (one layer, a small batch) their chunks are many, and a lone warp would take them one latency after another.
+template <int V, bool kBf16, int kWarps>
 __global__ void __launch_bounds__(256)
 shared_join_kernel(const __grid_constant__ SharedParams p)
 {
     griddep_wait();
     griddep_launch_dependents();
     constexpr int D = V * 32, kBatch = 8;
-    const int lane = threadIdx.x & 31;
+    __shared__ float2 s_ml[8];
+    __shared__ float s_o[8][D];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = warp % kWarps;
     const long long rows = (long long)p.num_gated * p.batch * p.num_q_heads;
     const SharedDesc& sd = *p.desc;
     const int t1 = sd.t1, nseg = sd.nseg;
     const long long total = sd.total;
-    for (long long w = ((long long)blockIdx.x * blockDim.x + threadIdx.x) >> 5; w < rows;
-         w += ((long long)gridDim.x * blockDim.x) >> 5) {
+    // (with kWarps = 8 a CTA has one row at a time, and its warps agree on every branch but the last)
+    for (long long w = ((long long)blockIdx.x * 8 + warp) / kWarps; w < rows; w += (long long)gridDim.x * 8 / kWarps) {
         const int h = (int)(w % p.num_q_heads);
         const int b = (int)((w / p.num_q_heads) % p.batch);
         const int gl = (int)(w / ((long long)p.num_q_heads * p.batch));
         if (!p.flags[b] || p.seq_lens[b] < 1) continue;
         const int layer = p.layer[gl];
         const SharedRow r = sd.rows[b];
-        const size_t tail = ((size_t)(layer - p.layer_begin) * p.batch + b) * p.num_q_heads + h;
-        float2 ml = p.tail_ml[tail];
+        float2 ml = make_float2(-INFINITY, 0.f);
         float o[V];
 #pragma unroll
-        for (int e = 0; e < V; ++e) o[e] = p.tail_o[tail * D + lane * V + e];
+        for (int e = 0; e < V; ++e) o[e] = 0.f;
+        if (sub == 0) {
+            const size_t tail = ((size_t)(layer - p.layer_begin) * p.batch + b) * p.num_q_heads + h;
+            ml = p.tail_ml[tail];
+#pragma unroll
+            for (int e = 0; e < V; ++e) o[e] = p.tail_o[tail * D + lane * V + e];
+        }
         if (r.tiles > 0) {
             const int kvh = h / p.group;
             const long long u0 = ((long long)gl * p.num_kv_heads + kvh) * t1 + r.unit;
             const int j0 = (int)(((u0 + 1) * nseg - 1) / total);             // the spans of its first and last tile
             const int j1 = (int)(((u0 + r.tiles) * nseg - 1) / total);
+            const int chunks = (j1 - j0 + 1) * r.copies, per_copy = kShRows / r.copies;
             const size_t ext = p.ext_row0 + r.row + (h - kvh * p.group);
-            for (int c0 = j0; c0 <= j1; c0 += kBatch) {
+            for (int c0 = sub; c0 < chunks; c0 += kBatch * kWarps) {
                 float2 cm[kBatch];
                 float co[kBatch][V];
 #pragma unroll
-                for (int c = 0; c < kBatch; ++c) {
-                    const int j = c0 + c;
-                    if (j > j1) {
-                        cm[c] = make_float2(-INFINITY, 0.f);
+                for (int k = 0; k < kBatch; ++k) {
+                    const int c = c0 + k * kWarps;
+                    if (c >= chunks) {
+                        cm[k] = make_float2(-INFINITY, 0.f);
 #pragma unroll
-                        for (int e = 0; e < V; ++e) co[c][e] = 0.f;
+                        for (int e = 0; e < V; ++e) co[k][e] = 0.f;
                         continue;
                     }
-                    const size_t row = j == j0 ? (size_t)w : ext + (size_t)j * 256;
-                    cm[c] = p.part_ml[row];
+                    const int j = c / r.copies, copy = c - j * r.copies;
+                    const size_t row = j == 0 ? copy * (size_t)rows + w : ext + (size_t)(j0 + j) * 256 + copy * per_copy;
+                    cm[k] = p.part_ml[row];
 #pragma unroll
-                    for (int e = 0; e < V; ++e) co[c][e] = p.part_o[row * D + lane * V + e];
+                    for (int e = 0; e < V; ++e) co[k][e] = p.part_o[row * D + lane * V + e];
                 }
                 float m = ml.x;
 #pragma unroll
-                for (int c = 0; c < kBatch; ++c) m = fmaxf(m, cm[c].x);
+                for (int k = 0; k < kBatch; ++k) m = fmaxf(m, cm[k].x);
                 const float mu = m == -INFINITY ? 0.f : m;
                 const float a = ex2(ml.x - mu);
                 ml = make_float2(m, ml.y * a);
 #pragma unroll
                 for (int e = 0; e < V; ++e) o[e] *= a;
 #pragma unroll
-                for (int c = 0; c < kBatch; ++c) {
-                    const float f = ex2(cm[c].x - mu);
-                    ml.y += cm[c].y * f;
+                for (int k = 0; k < kBatch; ++k) {
+                    const float f = ex2(cm[k].x - mu);
+                    ml.y += cm[k].y * f;
 #pragma unroll
-                    for (int e = 0; e < V; ++e) o[e] = fmaf(co[c][e], f, o[e]);
+                    for (int e = 0; e < V; ++e) o[e] = fmaf(co[k][e], f, o[e]);
                 }
+            }
+        }
+        if constexpr (kWarps > 1) {
+            __syncthreads();                  // (the row before has been read)
+            if (lane == 0) s_ml[warp] = ml;
+#pragma unroll
+            for (int e = 0; e < V; ++e) s_o[warp][lane * V + e] = o[e];
+            __syncthreads();
+            if (sub != 0) continue;
+            float m = -INFINITY;
+#pragma unroll
+            for (int k = 0; k < kWarps; ++k) m = fmaxf(m, s_ml[k].x);
+            const float mu = m == -INFINITY ? 0.f : m;
+            ml = make_float2(m, 0.f);
+#pragma unroll
+            for (int e = 0; e < V; ++e) o[e] = 0.f;
+#pragma unroll
+            for (int k = 0; k < kWarps; ++k) {
+                const float f = ex2(s_ml[k].x - mu);
+                ml.y += s_ml[k].y * f;
+#pragma unroll
+                for (int e = 0; e < V; ++e) o[e] = fmaf(s_o[k][lane * V + e], f, o[e]);
             }
         }
         const float inv = 1.f / ml.y;
@@ -792,15 +879,19 @@ shared_join_kernel(const __grid_constant__ SharedParams p)
     }
 }
 
-cudaError_t launch_shared_join(const SharedParams& p, int head_dim, bool out_bf16, cudaStream_t st, bool pdl)
+template <int V, bool kBf16>
+static cudaError_t launch_join_t(const SharedParams& p, cudaStream_t st, bool pdl)
 {
     const long long rows = (long long)p.num_gated * p.batch * p.num_q_heads;
-    const dim3 grid((unsigned)std::min<long long>((rows + 7) / 8, 148 * 8));
-    if (head_dim == 128)
-        return out_bf16 ? launch_ex(shared_join_kernel<4, true>, grid, dim3(256), 0, st, pdl, p)
-                        : launch_ex(shared_join_kernel<4, false>, grid, dim3(256), 0, st, pdl, p);
-    return out_bf16 ? launch_ex(shared_join_kernel<2, true>, grid, dim3(256), 0, st, pdl, p)
-                    : launch_ex(shared_join_kernel<2, false>, grid, dim3(256), 0, st, pdl, p);
+    if (rows <= 148 * 8)  // a CTA per row, all resident
+        return launch_ex(shared_join_kernel<V, kBf16, 8>, dim3((unsigned)rows), dim3(256), 0, st, pdl, p);
+    return launch_ex(shared_join_kernel<V, kBf16, 1>, dim3((unsigned)std::min<long long>((rows + 7) / 8, 148 * 16)), dim3(256), 0, st, pdl, p);
+}
+
+cudaError_t launch_shared_join(const SharedParams& p, int head_dim, bool out_bf16, cudaStream_t st, bool pdl)
+{
+    if (head_dim == 128) return out_bf16 ? launch_join_t<4, true>(p, st, pdl) : launch_join_t<4, false>(p, st, pdl);
+    return out_bf16 ? launch_join_t<2, true>(p, st, pdl) : launch_join_t<2, false>(p, st, pdl);
 }
 
 template <int D, int kTerms, bool kWide>

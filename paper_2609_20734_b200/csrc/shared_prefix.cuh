@@ -13,11 +13,11 @@ struct __align__(16) SharedRow {   // one request
     int32_t unit;    // first tile of its row block within one (layer, kv head)
     int32_t tiles;   // tiles of its prefix (0: it shares nothing)
     int32_t row;     // its first row within the row block
-    int32_t pad;
+    int32_t copies;  // partial results of each of its rows per chunk (see row_copies)
 };
 
-// Partial results of a row over its prefix: chunk 0 at row ((gated layer) * batch + b) * q_heads + head, chunk c > 0 at
-// ext_row0 + (first span + c) * 256 + row + head within the group.
+// Partial results of a row over its prefix: chunk 0 at row (copy * gated layers + gated layer) * batch * q_heads + b *
+// q_heads + head, chunk c > 0 at ext_row0 + (first span + c) * 256 + copy * (128 / copies) + row + head within the group.
 struct SharedDesc {
     int32_t t1, total, nseg, pad;    // tiles of one (layer, kv head), of all, spans they are cut into
     int32_t gated_index[kMaxLayers]; // layer -> its place among the call's gated layers
