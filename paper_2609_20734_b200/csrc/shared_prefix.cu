@@ -53,15 +53,13 @@ struct ShCfg {
     static constexpr int kTilePages = kTokens / kPage;
     static constexpr int kTileBytes = kTokens * D * 2;      // K or V of one tile
     static constexpr int kSlotBytes = 2 * kTileBytes;       // V of a tile, and behind it the K that is needed next
-    static constexpr int kRing = kWide ? 131072 : 180224;
-    static constexpr int kSlots = kRing / kSlotBytes;
+    static constexpr int kSlots = (kWide ? 131072 : 196608) / kSlotBytes;
+    static constexpr int kRingSlots = kSlots / 2;           // slots of one stream's ring
+    static_assert(kSlots % 2 == 0, "a stream and a producer keep to the slots of one parity");
     static constexpr int kQBytes = kShRows * D * 2;
     static constexpr int kQTiles = kWide ? 2 : 1;
     static constexpr int kSpCols = kTokens / 2 * kTerms > kTokens ? kTokens / 2 * kTerms : kTokens;  // one S, then P
-    static constexpr int kBufs = 4 * kSpCols + 2 * D <= 512 ? 2 : 1;
-    // tiles that K runs ahead of V: those whose S there is room for
-    static constexpr int kAhead = 2 * kBufs;                // streams in turn
-    static constexpr int kAheadDual = kBufs;                // both streams on every tile
+    static constexpr int kBufs = 4 * kSpCols + 2 * D <= 512 ? 2 : 1;  // and the tiles that a stream's K runs ahead of its V
     static constexpr int kO0 = 2 * kBufs * kSpCols;         // first column of stream 0's O
     static constexpr int kRowBlock = kWide ? 256 : 128;     // rows of a unit
     static_assert(kO0 + 2 * D <= 512, "TMEM");
@@ -81,7 +79,6 @@ struct ShCtl {
     uint64_t ml_full, o1_read;       // joining the streams: stream 1's (m, l) are there, its O has been read
     uint32_t tmem;
     int32_t abort;
-    float2 ml1[kShRows];             // stream 1's (m, l) when the streams are joined
 };
 
 // Few rows leave most of a 128-row tile, and most of the softmax warps, idle.  The tile then holds every row 2 or 4 times
@@ -166,6 +163,17 @@ __device__ __forceinline__ void tc_ld16(uint32_t addr, float* v)
         : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
           "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
         : "r"(addr));
+}
+__device__ __forceinline__ void tc_st2(uint32_t addr, const uint32_t* r)
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x2.b32 [%0], {%1,%2};" ::"r"(addr), "r"(r[0]), "r"(r[1]) : "memory");
+}
+__device__ __forceinline__ float2 tc_ld2(uint32_t addr)
+{
+    uint32_t a, b;
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x2.b32 {%0,%1}, [%2];" : "=r"(a), "=r"(b) : "r"(addr));
+    tc_wait_ld();
+    return make_float2(__uint_as_float(a), __uint_as_float(b));
 }
 __device__ __forceinline__ void tc_st8(uint32_t addr, const uint32_t* r)
 {
@@ -316,6 +324,24 @@ __device__ __forceinline__ ShItem shared_item(const SharedParams& p, const ShPla
     return it;
 }
 
+// The ring.  Where both streams use every tile ("dual", wide form), positions i = 0, 1, ... of an item go to slots 0, 1, ...
+// around all kSlots; where they take tiles in turn, stream s has the slots of parity s to itself, position i of ITS
+// tiles in slot 2 (i mod kSlots / 2) + s.  A stream's first positions hold the K tiles that run ahead of V alone, the
+// rest V of a tile with the K that comes next.  Every item begins at its first slots; `parity` has a bit per slot for
+// how often it has been filled.  So each slot is filled by one producer warp, and whoever waits for a filling has
+// seen the one before (or is joined with who has): a wait by parity cannot be answered by an older phase.
+template <int kSlots>
+__device__ __forceinline__ uint32_t ring_after(uint32_t parity, bool dual, int pos0, int pos1)
+    {
+#pragma unroll
+    for (int i = 0; i < kSlots; ++i) {
+        const int n = dual ? (pos0 + kSlots - 1 - i) / kSlots
+                           : ((i & 1 ? pos1 : pos0) + kSlots / 2 - 1 - i / 2) / (kSlots / 2);  // fillings of slot i
+        parity ^= (uint32_t)(n & 1) << i;
+    }
+    return parity;
+}
+
 template <int D, int kTerms, bool kWide>
 __global__ void __launch_bounds__(384, 1)
 shared_prefix_kernel(const __grid_constant__ SharedParams p, const __grid_constant__ CUtensorMap kmap,
@@ -332,7 +358,7 @@ shared_prefix_kernel(const __grid_constant__ SharedParams p, const __grid_consta
     volatile int* abort_flag = &ctl.abort;
     if (tid == 0) {
         for (int s = 0; s < C::kSlots; ++s) {
-            mbar_init(smem_u32(&ctl.full[s]), 2);
+            mbar_init(smem_u32(&ctl.full[s]), 1);
             mbar_init(smem_u32(&ctl.empty[s]), kWide ? 2 : 1);
         }
         for (int s = 0; s < 2; ++s) {
@@ -371,19 +397,19 @@ shared_prefix_kernel(const __grid_constant__ SharedParams p, const __grid_consta
     if constexpr (kWide) asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
     if (warp == 8 || warp == 11) {
         // ============================ producer warps ============================
-        // Each issues half of every slot's boxes: a warp spends about 125 cycles on a box, and the 12 boxes of
-        // a 64-position tile (1,400 cycles of DRAM's time) were more than one warp could issue.
+        // Warp 8 fills the even slots, warp 11 the odd ones: a warp spends about 110 cycles on a box and 350 more on a
+        // slot, and DRAM delivers the 12 boxes of a slot (64 positions, D = 128) in 1,400.
         const int half = warp == 8 ? 0 : 1;
         const uint64_t once = 0x12F0000000000000ull;    // L2 evict-first: read by one row block
         const uint64_t again = 0x1000000000000000ull;   // L2 evict-normal: the next row block reads it too
-        uint32_t cnt = 0;
-        bool dead = false;
-        for (int x = x0; x < x1 && !dead;) {
+        uint32_t parity = 0;
+        bool ok = true;
+        for (int x = x0; x < x1 && ok;) {
             const ShItem it = shared_item<TP, C::kRowBlock>(p, pl, x, x1);
             x += it.n;
-            const int ahead = kWide && it.nrows > kShRows ? C::kAheadDual : C::kAhead;
-            const int lead = pl.g.list[pl.g.gs[it.group]];
-            const int32_t* table = p.block_table + (size_t)lead * p.max_blocks_per_seq;
+            const bool dual = kWide && it.nrows > kShRows;
+            const int lead_req = pl.g.list[pl.g.gs[it.group]];
+            const int32_t* table = p.block_table + (size_t)lead_req * p.max_blocks_per_seq;
             const int first = it.tile0 * TP, last = min(it.pages, (it.tile0 + it.n) * TP);
             const int kv0 = p.kv_index[it.gl] * p.blocks_per_layer;
             const uint64_t policy = pl.g.members[it.group] * p.group > C::kRowBlock ? again : once;
@@ -401,43 +427,43 @@ shared_prefix_kernel(const __grid_constant__ SharedParams p, const __grid_consta
                 }
                 return kv0 + __shfl_sync(0xffffffffu, id.now, (pg - id.base + pgi) & 31);
             };
-            // one slot: V of tile tv and K of tile tk (-1: none)
-            auto load = [&](int tv, int tk) {
-                const uint32_t s = cnt % C::kSlots, ph = (cnt / C::kSlots) & 1;
-                if (!warp_wait(&ctl.empty[s], ph ^ 1, abort_flag, p.status)) return false;
-                const uint32_t bar = smem_u32(&ctl.full[s]), dst = smem_u32(ring + s * C::kSlotBytes);
-                constexpr int kEach = kSlabs * TP / 2;
-                const int vi = half * (TP / 2) + lane, ke = half * kEach + lane, ki = ke % TP, slab = ke / TP;
-                bool mv = false, mk = false;
-                int bv = 0, bk = 0;
-                if (tv >= 0) {  // one box: the page of the head, slab after slab
-                    const int pg = first + tv * TP;
-                    mv = lane < TP / 2 && pg + vi < last;
-                    bv = block_of(ids_v, pg, vi);
-                }
-                if (tk >= 0) {  // one box per slab: a slab's rows of all pages lie one behind the other
-                    const int pg = first + tk * TP;
-                    mk = lane < kEach && pg + ki < last;
-                    bk = block_of(ids_k, pg, ki);
-                }
+            // one slot: V of tile tv and K of tile tk (-1: none).  Lanes 0 .. TP-1 take a page of V each (one box: the page
+            // of the head, slab after slab), lanes 8 and up a page and slab of K (a slab's rows of all pages lie one
+            // behind the other).
+            auto load = [&](int tv, int tk, int slot, int round) {
+                const int e = lane - 8, ki = e % TP, slab = e / TP;
+                const int bv = tv >= 0 ? block_of(ids_v, first + tv * TP, lane) : 0;
+                const int bk = tk >= 0 ? block_of(ids_k, first + tk * TP, ki) : 0;
+                const bool mv = tv >= 0 && lane < TP && first + tv * TP + lane < last;
+                const bool mk = tk >= 0 && e >= 0 && e < kSlabs * TP && first + tk * TP + ki < last;
                 const uint32_t bytes = __popc(__ballot_sync(0xffffffffu, mv)) * (kPage * D * 2) + __popc(__ballot_sync(0xffffffffu, mk)) * (kPage * 128);
+                if (!warp_wait(&ctl.empty[slot], ((parity >> slot) ^ (uint32_t)round ^ 1u) & 1u, abort_flag, p.status)) return false;
+                const uint32_t bar = smem_u32(&ctl.full[slot]), dst = smem_u32(ring + slot * C::kSlotBytes);
                 if (lane == 0) mbar_expect_tx(bar, bytes);
                 __syncwarp();
-                if (mv) tma_box(dst + vi * (kPage * D * 2), &vmap, bar, 0, it.kvh, bv, policy);
-                if (mk) tma_box(dst + C::kTileBytes + slab * (TN * 128) + ki * 2048, &kmap, bar, slab, it.kvh, bk, policy);
-                ++cnt;
+                if (mv || mk)
+                    tma_box(mv ? dst + lane * (kPage * D * 2) : dst + C::kTileBytes + slab * (TN * 128) + ki * 2048, mv ? &vmap : &kmap, bar,
+                            mv ? 0 : slab, it.kvh, mv ? bv : bk, policy);
                 return true;
             };
-            bool ok = true;
-            for (int t = 0; t < min(ahead, it.n) && ok; ++t) ok = load(-1, t);
-            for (int t = 0; t < it.n && ok; ++t) ok = load(t, t + ahead < it.n ? t + ahead : -1);
-            dead = !ok;
+            // the positions of the slots that are this warp's: of the item (dual: every other one), or of its stream's tiles
+            const int step = dual ? 1 : 2, t0 = dual ? 0 : half;
+            const int nt = t0 < it.n ? (it.n - t0 + step - 1) / step : 0, lead = min(C::kBufs, nt);
+            int slot = half, round = 0;
+            for (int i = dual ? half : 0; i < lead + nt && ok; i += dual ? 2 : 1) {
+                const int j = i - lead;     // of the stream's tiles: V of the j-th, K of the (j + kBufs)-th
+                ok = load(j >= 0 ? t0 + j * step : -1, j < 0 ? t0 + i * step : j + C::kBufs < nt ? t0 + (j + C::kBufs) * step : -1, slot, round);
+                slot += 2;
+                if (slot >= C::kSlots) { slot = half; ++round; }
+            }
+            const int n1 = it.n / 2;        // (tiles of stream 1 where they take turns)
+            parity = dual ? ring_after<C::kSlots>(parity, true, lead + nt, 0)
+                          : ring_after<C::kSlots>(parity, false, it.n - n1 + min(C::kBufs, it.n - n1), n1 + min(C::kBufs, n1));
         }
-        // do not leave while copies may still be landing: every armed slot has been released (bounded)
-        for (uint32_t k = 0; k < (uint32_t)C::kSlots && k < cnt; ++k) {
-            const uint32_t c2 = cnt - 1 - k;
-            if (!warp_wait(&ctl.empty[c2 % C::kSlots], (c2 / C::kSlots) & 1, abort_flag, p.status)) break;
-        }
+        // Do not leave while copies may still be landing: every slot of this warp has been released since it was last
+        // filled (bounded; a slot that was never filled answers at once).
+        for (int slot = half; slot < C::kSlots && ok; slot += 2)
+            ok = warp_wait(&ctl.empty[slot], ((parity >> slot) & 1u) ^ 1u, abort_flag, p.status);
     } else {
         // ============================ MMA warps: one per stream, one thread issues ============================
         // (The loop is run by the whole warp on warp-uniform values, and descriptors differ by constants: a thread
@@ -450,7 +476,7 @@ shared_prefix_kernel(const __grid_constant__ SharedParams p, const __grid_consta
         const uint32_t sp0 = tm + s * C::kBufs * C::kSpCols, to = tm + C::kO0 + s * D;  // S, then P; O
         const uint32_t q_lo = smem_lo(smem_u32(qs), 16) + (kWide ? s : 0) * (C::kQBytes >> 4);
         const uint32_t k_lo = smem_lo(smem_u32(ring) + C::kTileBytes, 16), v_lo = smem_lo(smem_u32(ring), 2048);
-        uint32_t base = 0;               // slots before the item
+        uint32_t parity = 0;
         uint32_t nq = 0, np[2] = {0, 0};
         bool ok = true;
         for (int x = x0; x < x1 && ok;) {
@@ -459,15 +485,16 @@ shared_prefix_kernel(const __grid_constant__ SharedParams p, const __grid_consta
             const int n = __shfl_sync(0xffffffffu, item.n, 0);
             const bool dual = kWide && __shfl_sync(0xffffffffu, item.nrows, 0) > kShRows;
             const int rest = __shfl_sync(0xffffffffu, item.pages - item.tile0 * TP, 0);  // pages from the item's first on
-            const int ahead = dual ? C::kAheadDual : C::kAhead, lead = min(ahead, n);
             const int step = dual ? 1 : 2, t0 = dual ? 0 : s;     // the stream's tiles: t0, t0 + step, ...
             const int nt = t0 < n ? (n - t0 + step - 1) / step : 0;
             constexpr int bufs = C::kBufs;
-            // slots in the producers' order: K_0 .. K_(lead-1) alone, then V_t with K_(t+ahead)
-            uint32_t slot = 0, phase = 0;
-            auto go_to = [&](uint32_t at) { slot = at % C::kSlots; phase = (at / C::kSlots) & 1; };
+            int slot = dual ? 0 : s, round = 0;
+            auto next_slot = [&]() {
+                slot += step;
+                if (slot >= C::kSlots) { slot = dual ? 0 : s; ++round; }
+            };
             auto acquire = [&]() {
-                ok = warp_wait(&ctl.full[slot], phase, abort_flag, p.status);
+                ok = warp_wait(&ctl.full[slot], ((parity >> slot) ^ (uint32_t)round) & 1u, abort_flag, p.status);
                 tc_fence_after();
             };
             auto release = [&]() {             // in the wide form a slot is free after two arrivals: one of each stream,
@@ -485,20 +512,18 @@ shared_prefix_kernel(const __grid_constant__ SharedParams p, const __grid_consta
                     tc_commit(smem_u32(&ctl.s_full[s][u]));
                 }
             };
-            // narrow: one copy of Q, loaded by stream 0 for every item; wide: each stream's own, where it has a tile
-            if (!kWide || nt > 0) {
-                ok = warp_wait(&ctl.q_full[kWide ? s : 0], nq++ & 1, abort_flag, p.status);
+            if (nt > 0) {
+                ok = warp_wait(&ctl.q_full[s], nq++ & 1, abort_flag, p.status);
                 if (!ok) break;
                 tc_fence_after();
             }
             for (int i = 0; i < min(bufs, nt); ++i) {
-                go_to(base + t0 + i * step);
                 acquire();
                 if (!ok) break;
                 qk(i);
                 release();
+                next_slot();
             }
-            go_to(base + lead + t0);
             for (int i = 0; i < nt && ok; ++i) {
                 const int u = bufs == 2 ? i & 1 : 0;
                 acquire();
@@ -528,10 +553,11 @@ shared_prefix_kernel(const __grid_constant__ SharedParams p, const __grid_consta
                     tc_commit(smem_u32(&ctl.pv_done[s][u]));
                 }
                 release();
-                slot += step;
-                if (slot >= C::kSlots) { slot -= C::kSlots; phase ^= 1; }
+                next_slot();
             }
-            base += lead + n;
+            const int n1 = n / 2;
+            parity = dual ? ring_after<C::kSlots>(parity, true, nt + min(bufs, nt), 0)
+                          : ring_after<C::kSlots>(parity, false, n - n1 + min(bufs, n - n1), n1 + min(bufs, n1));
         }
         __syncwarp();
     }
@@ -669,7 +695,10 @@ shared_prefix_kernel(const __grid_constant__ SharedParams p, const __grid_consta
             if (kWide || s == 0) {
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
-                if (lane == 0) mbar_arrive(smem_u32(&ctl.q_full[s]));
+                if (lane == 0) {
+                    mbar_arrive(smem_u32(&ctl.q_full[s]));
+                    if (!kWide && it.n > 1) mbar_arrive(smem_u32(&ctl.q_full[1]));  // one copy for both streams
+                }
             }
             m = -INFINITY;
             l = 0.f;
@@ -703,14 +732,16 @@ shared_prefix_kernel(const __grid_constant__ SharedParams p, const __grid_consta
             float a0 = 1.f, a1 = 0.f;
             if (joined) {
                 if (s == 1) {
-                    ctl.ml1[tr] = make_float2(m, l);
+                    const uint32_t v[2] = {__float_as_uint(m), __float_as_uint(l)};  // left in its own, now unused, S
+                    tc_st2(sp0, v);
+                    tc_wait_st();
                     tc_fence_before();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(smem_u32(&ctl.ml_full));
                 } else {
                     if (!warp_wait(&ctl.ml_full, nj & 1, abort_flag, p.status)) { ok = false; break; }
                     tc_fence_after();
-                    const float2 o = ctl.ml1[tr];
+                    const float2 o = tc_ld2(sp0 + C::kBufs * C::kSpCols);
                     const float mn = fmaxf(m, o.x), mu = mn == -INFINITY ? 0.f : mn;
                     a0 = ex2(m - mu);
                     a1 = ex2(o.x - mu);

@@ -192,3 +192,20 @@ def test_shared_large_logits():
     # keys are six times longer: so are logits and their errors
     assert np.abs(out.cpu().numpy() - ref).max() <= 6 * gh.ATOL_OUT
     assert np.abs(lse.cpu().numpy() - rlse).max() <= 6 * gh.ATOL_LSE
+
+
+@pytest.mark.parametrize("D,Hq,Hkv,B,dtype", [(128, 16, 8, 3, 1), (64, 16, 8, 3, 0), (64, 8, 8, 12, 1), (128, 64, 8, 17, 1), (64, 64, 8, 20, 0)])
+def test_shared_long_runs_through_the_ring(D, Hq, Hkv, B, dtype):
+    """Prefixes long enough, over enough heads and layers, that every CTA goes around its ring of tiles many times in one
+    piece of work and through several pieces, with rows for one and for two row tiles."""
+    L, prefix = (6, 3200) if B < 17 else (2, 3200)
+    seq = [prefix + 1 + (5 * i) % 37 for i in range(B)]
+    prob = make_problem(900 + D + B, L, B, Hq, Hkv, D, seq)
+    share_prefixes(prob, [0, B], [prefix])
+    ctx, out, lse = run_shared(prob, [0, B], [prefix], [1] * B, dtype=dtype)
+    assert ctx.read_device_status() == 0
+    # some requests, all heads and layers
+    some = [0, 1, B - 1]
+    few = dict(prob, B=len(some), q=prob["q"][:, some], table=prob["table"][some], seq_lens=prob["seq_lens"][some])
+    ref, rlse, _ = full_reference(few)
+    rows_close(out[:, some], lse[:, some], ref, rlse, range(L), range(len(some)), "long runs")
