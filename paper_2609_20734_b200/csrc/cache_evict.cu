@@ -27,13 +27,20 @@ constexpr int kSelMost = 47104;       // and at most (184 KiB; longer parts are 
 constexpr int kCopies = 4;            // of a CTA's histogram: lanes that count the same digit (most weights share a few
                                       // exponents) rarely meet in one word
 
-// Weights are held as their bits with -0 as 0 and every NaN as the largest positive pattern, so that the key is two
-// instructions: larger weight, larger key; -0 and 0 are one, NaN is above everything.
-__device__ __forceinline__ uint32_t weight_bits(float w)
+// Weights are held as order-preserving keys: larger weight, larger key; -0 and 0 are one, NaN (any) is above everything.
+__device__ __forceinline__ uint32_t weight_key(float w)
 {
-    return w != w ? 0x7fffffffu : __float_as_uint(w + 0.f);
+    const uint32_t u = w != w ? 0x7fffffffu : __float_as_uint(w + 0.f);
+    return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
 }
-__device__ __forceinline__ uint32_t weight_key(uint32_t u) { return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u); }
+__device__ __forceinline__ float key_weight(uint32_t k) { return __uint_as_float(k ^ ((uint32_t)((int32_t)~k >> 31) | 0x80000000u)); }
+constexpr uint32_t kZeroKey = 0x80000000u;
+
+// one more at a shared-memory word, if `when` (predicated: a branch per position costs more than all its arithmetic)
+__device__ __forceinline__ void shared_inc(uint32_t addr, bool when)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %1, 0;\n\t@p red.shared.add.u32 [%0], 1;\n\t}" ::"r"(addr), "r"((uint32_t)when) : "memory");
+}
 
 __device__ __forceinline__ uint32_t cluster_rank()
 {
@@ -76,7 +83,7 @@ evict_select_kernel(const __grid_constant__ EvictParams p, const int nc)
 {
     griddep_wait();
     griddep_launch_dependents();
-    extern __shared__ __align__(16) uint32_t part[];  // this CTA's positions of the round: weight_bits
+    extern __shared__ __align__(16) uint32_t part[];  // this CTA's positions of the round: their keys
     constexpr int kSelWarps = kSelThreads / 32;
     __shared__ SelShared<kSelWarps> sh;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -113,10 +120,10 @@ evict_select_kernel(const __grid_constant__ EvictParams p, const int nc)
         for (int i = tid; i < m / 4; i += 2 * kSelThreads) {
             const bool two = i + kSelThreads < m / 4;
             const float4 x = __ldcg(from + i), y = two ? __ldcg(from + i + kSelThreads) : x;
-            to[i] = make_uint4(weight_bits(x.x), weight_bits(x.y), weight_bits(x.z), weight_bits(x.w));
-            if (two) to[i + kSelThreads] = make_uint4(weight_bits(y.x), weight_bits(y.y), weight_bits(y.z), weight_bits(y.w));
+            to[i] = make_uint4(weight_key(x.x), weight_key(x.y), weight_key(x.z), weight_key(x.w));
+            if (two) to[i + kSelThreads] = make_uint4(weight_key(y.x), weight_key(y.y), weight_key(y.z), weight_key(y.w));
         }
-        if (tid < m % 4) part[m / 4 * 4 + tid] = weight_bits(__ldcg(w + i0 + m / 4 * 4 + tid));
+        if (tid < m % 4) part[m / 4 * 4 + tid] = weight_key(__ldcg(w + i0 + m / 4 * 4 + tid));
         return m;
     };
     if (tid < 256)
@@ -131,16 +138,14 @@ evict_select_kernel(const __grid_constant__ EvictParams p, const int nc)
         for (int pass = 0; pass < 4; ++pass) {
             const int shift = 24 - 8 * pass;
             const uint32_t above = pass == 0 ? 0u : 0xffffffffu << (shift + 8);
-            uint32_t* hist = sh.hist[lane % kCopies];
+            const uint32_t hist = smem_u32(sh.hist[lane % kCopies]);
             // (weights of 0 -- positions nobody looked at -- are one key and may be most of them: they are counted apart,
             // in the first pass)
             uint32_t zeros = 0;
-            auto count = [&](uint32_t u) {
-                const uint32_t k = weight_key(u);
-                if (u == 0)
-                    ++zeros;
-                else if ((k & above) == prefix)
-                    atomicAdd(&hist[(k >> shift) & 255u], 1u);
+            auto count = [&](uint32_t k) {
+                const bool zero = k == kZeroKey;
+                zeros += zero;
+                shared_inc(hist + ((k >> shift) & 255u) * 4, ((k ^ prefix) & above) == 0 && !zero);
             };
             if (rounds == 1) {
                 const int i0 = rank * per;
@@ -157,7 +162,7 @@ evict_select_kernel(const __grid_constant__ EvictParams p, const int nc)
                     }
                 }
             } else {
-                for (int i = lo + rank * kSelThreads + tid; i < hi; i += nc * kSelThreads) count(weight_bits(__ldcg(w + i)));
+                for (int i = lo + rank * kSelThreads + tid; i < hi; i += nc * kSelThreads) count(weight_key(__ldcg(w + i)));
             }
             if (pass == 0) {
                 zeros = __reduce_add_sync(0xffffffffu, zeros);
@@ -171,7 +176,7 @@ evict_select_kernel(const __grid_constant__ EvictParams p, const int nc)
                     sum += sh.hist[k][tid];
                     sh.hist[k][tid] = 0;
                 }
-                if ((0x80000000u & above) == prefix && tid == (int)((0x80000000u >> shift) & 255u)) sum += sh.zeros;
+                if (((kZeroKey ^ prefix) & above) == 0 && tid == (int)((kZeroKey >> shift) & 255u)) sum += sh.zeros;
                 (nc == 1 ? sh.total : sh.sum[pass % 3])[tid] = sum;
             }
             if (nc > 1) {
@@ -215,7 +220,7 @@ evict_select_kernel(const __grid_constant__ EvictParams p, const int nc)
     }
     // ordered pass: heavier than T, or T itself while `left` of them last.  A warp owns a run of its CTA's part: it
     // counts, the counts before it are added up, and it goes over the run again with the places known.
-    const uint32_t T = prefix;
+    const uint32_t T = any ? prefix : 0xffffffffu;
     uint32_t base_gt = 0, base_eq = 0;
     for (int r = 0; r < rounds; ++r) {
         if (rounds > 1) {
@@ -225,24 +230,20 @@ evict_select_kernel(const __grid_constant__ EvictParams p, const int nc)
         const long long i0 = ((long long)r * nc + rank) * per;
         const int run = per / 128 / kSelWarps * 128 + 128;         // positions of one warp
         const int j0 = warp * run, j1 = min(m, j0 + run);
-        // of the four positions from j on: bits 0-3 heavier than T (or kept in any case), bits 4-7 of weight T
+        // of the four positions from j on: bits 0-3 heavier than T (or kept in any case), bits 4-7 of weight T.  Where no
+        // candidate stays T is the largest key and nothing equals it (`any` is off).
         auto classes = [&](int j, const uint4& u) {
-            const uint32_t k[4] = {weight_key(u.x), weight_key(u.y), weight_key(u.z), weight_key(u.w)};
+            const uint32_t k[4] = {u.x, u.y, u.z, u.w};
             uint32_t c = 0;
-            if (any) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) c |= (k[e] > T ? 1u << e : 0u) | (k[e] == T ? 16u << e : 0u);
-            }
-            const long long i = i0 + j;
-            if (i < lo || i + 4 > hi) {
+            for (int e = 0; e < 4; ++e) c |= (k[e] > T ? 1u << e : 0u) | (any && k[e] == T ? 16u << e : 0u);
+            const int i = (int)i0 + j;
+            if (i < lo || i + 4 > hi || j + 4 > j1) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
+                for (int e = 0; e < 4; ++e) {
                     if (i + e < lo || i + e >= hi) c = (c & ~(16u << e)) | (1u << e);
-            }
-            if (j + 4 > j1) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
                     if (j + e >= j1) c &= ~(17u << e);
+                }
             }
             return c;
         };
@@ -300,7 +301,7 @@ evict_select_kernel(const __grid_constant__ EvictParams p, const int nc)
                 if (lane >= o) x += y;
             }
             uint32_t my_gt = gts + ((x - own) & 0xffffu), my_eq = eqs + ((x - own) >> 16);
-            const uint32_t bits[4] = {u.x, u.y, u.z, u.w};
+            const uint32_t keys[4] = {u.x, u.y, u.z, u.w};
             int gone = 0x7fffffff;         // first of the four that is dropped
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
@@ -308,7 +309,7 @@ evict_select_kernel(const __grid_constant__ EvictParams p, const int nc)
                 if (gt || (eq && my_eq < left)) {
                     const uint32_t dst = my_gt + min(my_eq, left);
                     kept[dst] = (int32_t)(i0 + j + e);
-                    w[dst] = __uint_as_float(bits[e]);  // dst is not behind its source, and every weight of the round has been read
+                    w[dst] = key_weight(keys[e]);  // dst is not behind its source, and every weight of the round has been read
                 } else if (j + e < j1 && gone == 0x7fffffff) {
                     gone = (int)(i0 + j + e);
                 }
