@@ -799,7 +799,7 @@ shared_prefix_kernel(const __grid_constant__ SharedParams p, const __grid_consta
 }
 
 // kWarps warps per row of a flagged request: tail and prefix chunks joined by log-sum-exp, rounded once.  A warp takes its
-// chunks eight at a time, all their loads before the first use.  One warp is enough where rows are many; where they are
+// chunks 4 or 8 at a time, all their loads before the first use.  One warp is enough where rows are many; where they are
 // few (one layer, a small batch) their chunks are many, and a lone warp would take them one latency after another.
 template <int V, bool kBf16, int kWarps>
 __global__ void __launch_bounds__(256)
@@ -807,7 +807,7 @@ shared_join_kernel(const __grid_constant__ SharedParams p)
 {
     griddep_wait();
     griddep_launch_dependents();
-    constexpr int D = V * 32, kBatch = 8;
+    constexpr int D = V * 32, kBatch = kWarps == 1 ? 4 : 8;
     __shared__ float2 s_ml[8];
     __shared__ float s_o[8][D];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = warp % kWarps;
@@ -820,18 +820,20 @@ shared_join_kernel(const __grid_constant__ SharedParams p)
         const int h = (int)(w % p.num_q_heads);
         const int b = (int)((w / p.num_q_heads) % p.batch);
         const int gl = (int)(w / ((long long)p.num_q_heads * p.batch));
-        if (!p.flags[b] || p.seq_lens[b] < 1) continue;
         const int layer = p.layer[gl];
+        // What the row's chunks are, and its tail, asked for together before anything is looked at (one latency, not four)
+        const int flag = p.flags[b], t = p.seq_lens[b];
         const SharedRow r = sd.rows[b];
-        float2 ml = make_float2(-INFINITY, 0.f);
+        const size_t tail = ((size_t)(layer - p.layer_begin) * p.batch + b) * p.num_q_heads + h;
+        float2 ml = __ldcg(p.tail_ml + tail);
         float o[V];
 #pragma unroll
-        for (int e = 0; e < V; ++e) o[e] = 0.f;
-        if (sub == 0) {
-            const size_t tail = ((size_t)(layer - p.layer_begin) * p.batch + b) * p.num_q_heads + h;
-            ml = p.tail_ml[tail];
+        for (int e = 0; e < V; ++e) o[e] = __ldcg(p.tail_o + tail * D + lane * V + e);
+        if (!flag || t < 1) continue;   // (what was read is not used)
+        if (sub != 0) {
+            ml = make_float2(-INFINITY, 0.f);
 #pragma unroll
-            for (int e = 0; e < V; ++e) o[e] = p.tail_o[tail * D + lane * V + e];
+            for (int e = 0; e < V; ++e) o[e] = 0.f;
         }
         if (r.tiles > 0) {
             const int kvh = h / p.group;
