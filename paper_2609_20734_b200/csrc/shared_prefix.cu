@@ -234,7 +234,8 @@ __device__ __forceinline__ void tma_box(uint32_t dst, const CUtensorMap* map, ui
 __device__ __forceinline__ bool warp_wait(const uint64_t* bar, uint32_t parity, volatile int* abort_flag, int* status)
 {
     const uint32_t a = smem_u32(bar);
-    bool ok = false;
+    bool ok = mbar_try_wait(a, parity);
+    if (__all_sync(0xffffffffu, ok)) return true;  // (one uniform branch where the phase has passed: the loop costs 200 cycles more)
     for (int i = 0; i < 64 && !ok; ++i) ok = mbar_try_wait(a, parity);
     if (!ok) ok = mbar_wait(a, parity, abort_flag, status);
     return __all_sync(0xffffffffu, ok);
@@ -469,10 +470,10 @@ shared_prefix_kernel(const __grid_constant__ SharedParams p, const __grid_consta
         // (The loop is run by the whole warp on warp-uniform values, and descriptors differ by constants: a thread
         // that computes them anew before each product issues one in 100 cycles, slower than they run.  One warp for
         // both streams spent 1470 cycles on a tile of 64 positions, most of them on its barriers.)
-        const int s = warp - 9;
+        const int s = __reduce_max_sync(0xffffffffu, warp - 9);  // (a reduction's result is known to be uniform: descriptors stay in uniform registers)
         constexpr uint32_t idesc_s = idesc_bf16(TN, false), idesc_o = idesc_bf16(D, true);
         const bool leader = elect_one();
-        const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
+        const uint32_t tm = __reduce_max_sync(0xffffffffu, tmem);
         const uint32_t sp0 = tm + s * C::kBufs * C::kSpCols, to = tm + C::kO0 + s * D;  // S, then P; O
         const uint32_t q_lo = smem_lo(smem_u32(qs), 16) + (kWide ? s : 0) * (C::kQBytes >> 4);
         const uint32_t k_lo = smem_lo(smem_u32(ring) + C::kTileBytes, 16), v_lo = smem_lo(smem_u32(ring), 2048);
@@ -482,9 +483,9 @@ shared_prefix_kernel(const __grid_constant__ SharedParams p, const __grid_consta
         for (int x = x0; x < x1 && ok;) {
             const ShItem item = shared_item<TP, C::kRowBlock>(p, pl, x, x1);
             x += item.n;
-            const int n = __shfl_sync(0xffffffffu, item.n, 0);
-            const bool dual = kWide && __shfl_sync(0xffffffffu, item.nrows, 0) > kShRows;
-            const int rest = __shfl_sync(0xffffffffu, item.pages - item.tile0 * TP, 0);  // pages from the item's first on
+            const int n = __reduce_max_sync(0xffffffffu, item.n);
+            const bool dual = kWide && __reduce_max_sync(0xffffffffu, item.nrows) > kShRows;
+            const int rest = __reduce_max_sync(0xffffffffu, item.pages - item.tile0 * TP);  // pages from the item's first on
             const int step = dual ? 1 : 2, t0 = dual ? 0 : s;     // the stream's tiles: t0, t0 + step, ...
             const int nt = t0 < n ? (n - t0 + step - 1) / step : 0;
             constexpr int bufs = C::kBufs;
