@@ -425,7 +425,8 @@ evict_move_kernel(const __grid_constant__ EvictParams p, const int nc)
             }
         }
     }
-    // the CTA that comes last shortens the requests: nobody reads their lengths any more
+    // the CTA that comes last shortens the requests: nobody reads their lengths any more (every thread has read them above)
+    __syncthreads();
     if (tid == 0) {
         __threadfence();
         if (atomicAdd(p.done, 1) == (int)(gridDim.x * gridDim.y) - 1) {
