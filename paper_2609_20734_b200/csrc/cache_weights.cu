@@ -24,14 +24,15 @@ accumulate_weights_kernel(const __grid_constant__ WeightParams p)
 {
     griddep_wait();
     griddep_launch_dependents();
-    const int b = blockIdx.y / p.num_kv_heads, g = blockIdx.y - b * p.num_kv_heads;
+    const uint32_t unit = blockIdx.x / p.chunks, chunk = blockIdx.x - unit * p.chunks;  // (x: units may be more than 65,535)
+    const int b = unit / p.num_kv_heads, g = unit - b * p.num_kv_heads;
     if (!p.flags[b]) return;
     const size_t max_pos = (size_t)p.max_blocks_per_seq * kPage;
     const int t = (int)min((long long)p.seq_lens[b], (long long)max_pos);  // the attention kernel reports what is beyond
-    const int j0 = (int)blockIdx.x * (kAccThreads * kAccPerThread) + threadIdx.x;
+    const int j0 = (int)chunk * (kAccThreads * kAccPerThread) + threadIdx.x;
     if (j0 >= t) return;
-    const int first = p.first_layer[blockIdx.z];  // of the call's gated layers that use this slice
-    float* w = p.weights + (((size_t)p.slice[blockIdx.z] * p.max_batch + b) * p.num_kv_heads + g) * max_pos;
+    const int first = p.first_layer[blockIdx.y];  // of the call's gated layers that use this slice
+    float* w = p.weights + (((size_t)p.slice[blockIdx.y] * p.max_batch + b) * p.num_kv_heads + g) * max_pos;
     float acc[kAccPerThread];
 #pragma unroll
     for (int i = 0; i < kAccPerThread; ++i) acc[i] = j0 + i * kAccThreads < t ? w[j0 + i * kAccThreads] : 0.f;
@@ -71,11 +72,15 @@ accumulate_weights_kernel(const __grid_constant__ WeightParams p)
         if (j0 + i * kAccThreads < t) w[j0 + i * kAccThreads] = acc[i];
 }
 
-cudaError_t launch_accumulate_weights(const WeightParams& p, int n_slices, int group, cudaStream_t st, bool pdl)
+cudaError_t launch_accumulate_weights(const WeightParams& args, int n_slices, int group, cudaStream_t st, bool pdl)
 {
-    const long long max_pos = (long long)p.max_blocks_per_seq * kPage;
+    const long long max_pos = (long long)args.max_blocks_per_seq * kPage;
     const int per = kAccThreads * kAccPerThread;
-    const dim3 grid((unsigned)((max_pos + per - 1) / per), p.batch * p.num_kv_heads, n_slices);
+    WeightParams p = args;
+    p.chunks = (int32_t)((max_pos + per - 1) / per);
+    const long long x = (long long)p.chunks * p.batch * p.num_kv_heads;
+    if (x > 0x7fffffffll) return cudaErrorInvalidConfiguration;
+    const dim3 grid((unsigned)x, n_slices);
     switch (group) {
         case 1: return launch_ex(accumulate_weights_kernel<1>, grid, dim3(kAccThreads), 0, st, pdl, p);
         case 2: return launch_ex(accumulate_weights_kernel<2>, grid, dim3(kAccThreads), 0, st, pdl, p);

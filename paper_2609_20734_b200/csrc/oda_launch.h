@@ -73,7 +73,8 @@ struct WeightParams {
     const int32_t* seq_lens;
     const uint8_t* flags;
     int32_t batch, max_batch, num_kv_heads, max_blocks_per_seq;
-    // grid.z walks the cache slices that the launch's gated layers use: the slice, its first layer, and from
+    int32_t chunks;              // CTAs along a unit's positions (set by the launch)
+    // grid.y walks the cache slices that the launch's gated layers use: the slice, its first layer, and from
     // each layer the next one on the same slice (-1: none).  Layers count from the launch's first.
     int16_t first_layer[kWeightMaxLayers], next_layer[kWeightMaxLayers];
     uint16_t slice[kWeightMaxLayers];

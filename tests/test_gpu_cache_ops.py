@@ -304,3 +304,80 @@ def test_weights_then_eviction_then_a_step():
     ref, rlse, _ = full_reference(after)
     rows_close(out, lse, ref, rlse, [0, 1], [0, 1, 2], "after the eviction")
     assert ctx.read_device_status() == 0
+
+
+def test_weighted_more_units_than_a_grid_axis_holds():
+    """128 requests x 513 heads of one position each: every weight is 1 and every output its value row."""
+    B, H, D = 128, 513, 64
+    prob = make_problem(41, 1, 1, H, H, D, [1])
+    ctx = gh.make_ctx(dict(prob, table=np.zeros((B, 2), np.int32)), [16], [0], [1], max_batch=B)
+    dev = gh.upload(prob)
+    q = dev["q"].expand(1, B, H, D).contiguous()
+    table = torch.full((B, 2), int(prob["table"][0, 0]), dtype=torch.int32, device="cuda")
+    w = torch.zeros((1, B, H, 32), device="cuda")
+    out = torch.zeros((1, B, H, D), device="cuda")
+    ctx.full_decode_weighted(0, 1, B, q, dev["k"], dev["v"], table, torch.ones(B, dtype=torch.int32, device="cuda"),
+                             torch.ones(B, **ONES), w, out)
+    torch.cuda.synchronize()
+    assert ctx.read_device_status() == 0
+    # one term: e^(z - lse) is 1 up to the rounding of exp and of 1 / l, the value passes through parts of bf16 unchanged
+    assert (w[..., 0] - 1).abs().max() <= 1e-6 and (w[..., 1:] == 0).all()
+    lay = prob["layout"]
+    rows = np.stack([prob["v"][int(prob["table"][0, 0]) * lay.block_stride + h * lay.head_stride:][:D] for h in range(H)])
+    want = torch.from_numpy(synth.bf16_bits_to_f32(rows))
+    assert (out[0].cpu() - want).abs().max() <= 1e-6 * want.abs().max()
+
+
+def test_evict_on_a_side_stream_captured_and_replayed():
+    """The call on a stream of its own equals the one on the default stream; a captured one reads lengths, weights and the
+    mask on the device each time, and a second replay on shortened requests changes nothing."""
+    seq, budget = [700, 90, 333], 128
+    prob = make_problem(23, 2, 3, 2, 2, 64, seq)
+    w_host = weight_pattern("random", (2, 3, 2, prob["table"].shape[1] * 16), np.random.default_rng(8))
+    want = evict_reference(prob, w_host, budget, 4, 48, [1, 1, 0])
+    ctx = gh.make_ctx(prob, [16] * 2, [0] * 2, [1] * 2)
+    dev = gh.upload(prob)
+    w = torch.from_numpy(w_host).cuda()
+    m = torch.zeros(3, **ONES)
+    kept = torch.full((2, 3, 2, budget), -7, dtype=torch.int32, device="cuda")
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=side):
+        ctx.evict(3, w, dev["k"], dev["v"], dev["table"], dev["seq_lens"], budget, 4, 48, mask=m, kept=kept)
+    g.replay()  # nobody may be shortened yet
+    torch.cuda.synchronize()
+    assert dev["seq_lens"].tolist() == seq and (kept == -7).all()
+    m.copy_(torch.tensor([1, 1, 0]))
+    for _ in range(2):
+        g.replay()
+        torch.cuda.synchronize()
+        got = [dev["k"].view(torch.int16).cpu().numpy().view(np.uint16), dev["v"].view(torch.int16).cpu().numpy().view(np.uint16),
+               w.cpu().numpy(), dev["seq_lens"].cpu().numpy()]
+        for name, a, b in zip(("k", "v", "weights", "seq_lens"), got, want):
+            np.testing.assert_array_equal(a, b, err_msg=name)
+    dev2, w2 = gh.upload(prob), torch.from_numpy(w_host).cuda()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        ctx.evict(3, w2, dev2["k"], dev2["v"], dev2["table"], dev2["seq_lens"], budget, 4, 48, mask=m)
+    side.synchronize()
+    assert torch.equal(w, w2) and torch.equal(dev["k"].view(torch.int16), dev2["k"].view(torch.int16)) and \
+        torch.equal(dev["seq_lens"], dev2["seq_lens"])
+    assert ctx.read_device_status() == 0
+
+
+def test_weights_are_read_in_16_byte_pieces_or_refused():
+    prob = make_problem(24, 1, 1, 2, 1, 64, [40])
+    ctx = gh.make_ctx(prob, [16], [0], [1])
+    dev = gh.upload(prob)
+    n = prob["table"].shape[1] * 16
+    off = torch.zeros(n + 1, device="cuda")[1:]
+    with pytest.raises(binding.OdaError) as e:
+        ctx.evict(1, off, dev["k"], dev["v"], dev["table"], dev["seq_lens"], 20)
+    assert e.value.status == 1 and ctx.launch_count == 0
+    # (the weighted pass takes any fp32 address)
+    before = off.clone()
+    out, lse = gh.new_out(prob)
+    ctx.full_decode_weighted(0, 1, 1, dev["q"], dev["k"], dev["v"], dev["table"], dev["seq_lens"], torch.ones(1, **ONES), off, out, lse)
+    _, _, wts = full_reference(prob)
+    weights_close(off.view(1, 1, 1, n), before.view(1, 1, 1, n), wts, prob, [1], [1], what="odd address")
