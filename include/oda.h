@@ -34,6 +34,10 @@
  *   - Errors a host check can see return a status with nothing enqueued.  Problems
  *     only the device can see (seq_len < 1) set a sticky status word in the
  *     workspace, readable with oda_read_device_status(); the kernels never trap.
+ *     Its bits: 1 a seq_len below 1 or beyond the block table, 2 more work than
+ *     the kernels' 32-bit counts hold, 4 a wait inside a kernel ran out (results
+ *     are not valid), 8 a group of oda_full_decode_shared out of order or outside
+ *     the batch.
  *   - One context must not be used from two streams at once (the workspace is
  *     shared scratch).
  */
@@ -355,14 +359,15 @@ oda_status_t oda_full_decode_gated(oda_ctx_t* ctx, int32_t layer_begin, int32_t 
  *     pages of the prefix are read through the block table of the group's first flagged request (usually all rows of
  *     the table name the same pages; copies are fine).  A page that the prefix ends in, and everything behind it, is
  *     read through each request's own row, so every row must be complete.  Requests in no group share nothing.
- *     group_start must not fall and must stay within [0, batch]: a group that breaks this sets bit 3 of the device
+ *     group_start must not fall and must stay within [0, batch]: a group that breaks this sets 8 in the device
  *     status word and shares nothing (its results stay right).  A prefix longer than a flagged request is cut to
  *     what leaves that request one position of its own; negative ones count as 0.
  *   flags, out, lse: as in oda_full_decode_gated.  0 <= num_groups <= 128, empty groups
  *     allowed; with 0 both arrays may be NULL.
  *   scratch: device, 256-byte aligned, oda_full_decode_shared_scratch_bytes(ctx) bytes, used only during the call.
  * Groups, lengths and flags are read on the device: one captured graph serves every prefix and every gate.  Always
- * computes from scratch (options bit 1 has no effect).  TMA variant only.
+ * computes from scratch (options bit 1 has no effect), and a calibrated split is not used: work is claimed as SMs
+ * become free.  Three launches (one with num_groups = 0: the plain gated pass).  TMA variant only.
  */
 size_t oda_full_decode_shared_scratch_bytes(const oda_ctx_t* ctx);
 oda_status_t oda_full_decode_shared(oda_ctx_t* ctx, int32_t layer_begin, int32_t layer_end, int32_t batch,
@@ -381,8 +386,8 @@ oda_status_t oda_full_decode_shared(oda_ctx_t* ctx, int32_t layer_begin, int32_t
  *     the caller zeroes a request's part when it starts.  Positions >= t and other requests are left as they were.
  *   scratch: device, 256-byte aligned, at least oda_full_decode_weighted_scratch_bytes(ctx, 1, batch) bytes; with
  *     room for n layers the call takes n layers at a time (two launches each time).
- * No atomics: the same call gives the same bits.  Always computes from scratch (options bit 1 has no effect).
- * TMA variant only.
+ * Nothing is added up by atomics: the same call gives the same bits.  Always computes from scratch (options bit 1 has
+ * no effect), without a calibrated split.  TMA variant only.
  */
 size_t oda_full_decode_weighted_scratch_bytes(const oda_ctx_t* ctx, int32_t layers, int32_t batch);
 oda_status_t oda_full_decode_weighted(oda_ctx_t* ctx, int32_t layer_begin, int32_t layer_end, int32_t batch,
@@ -400,8 +405,9 @@ oda_status_t oda_full_decode_weighted(oda_ctx_t* ctx, int32_t layer_begin, int32
  *   kept (nullable): [slices][batch][kv_heads][budget] i32, the old position of every new one; a request within the
  *     budget gets 0 .. t-1 and then -1, a masked one is not written.  Without it the list needs scratch (device,
  *     256-byte aligned, oda_evict_scratch_bytes(ctx) suffices for every budget); with it scratch may be NULL.
- *   weights: as in oda_full_decode_weighted, 16-byte aligned (a kept -0 may become 0, a NaN another NaN).  All slices of the cache are treated, those of fixed-window layers too:
- *     choose `recent` at least as large as the largest window, and what a Local pass reads stays what it was.
+ *   weights: as in oda_full_decode_weighted, 16-byte aligned (a kept -0 may become 0, a NaN another NaN).  All slices
+ *     of the cache are treated, those of fixed-window layers too: choose `recent` at least as large as the largest
+ *     window, and what a Local pass reads stays what it was.
  * The rows move inside the request's own pages: no other request may use a page of a request that is shortened
  * (a shared prefix is copied before its first eviction).  Pages behind the budget are free afterwards; the block table
  * is not changed.  Requires 1 <= budget <= max_blocks_per_seq * 16 and 0 <= sinks + recent <= budget.  A request with

@@ -251,6 +251,9 @@ class OdaContext:
         st = self.lib.oda_create(ctypes.byref(ccfg), ctypes.byref(self._h))
         if st != 0:
             raise OdaError(st, "oda_create", self.lib.oda_status_string(st).decode())
+        idx = cfg.layer_kv_index
+        #: cache slices the layers use (1 + the largest kv_index)
+        self.kv_slices = cfg.num_layers if idx is None else max(int(i) for i in idx) + 1
         self.workspace = None
         if allocate_workspace:
             import torch
@@ -425,12 +428,6 @@ class OdaContext:
         import torch
 
         return torch.empty(self.lib.oda_evict_scratch_bytes(self._h), dtype=torch.uint8, device=device)
-
-    @property
-    def kv_slices(self) -> int:
-        """Cache slices the layers use (1 + the largest kv_index)."""
-        idx = self.cfg.layer_kv_index
-        return self.cfg.num_layers if idx is None else max(int(i) for i in idx) + 1
 
     def _check_weights(self, w):
         c = self.cfg

@@ -209,3 +209,41 @@ def test_shared_long_runs_through_the_ring(D, Hq, Hkv, B, dtype):
     few = dict(prob, B=len(some), q=prob["q"][:, some], table=prob["table"][some], seq_lens=prob["seq_lens"][some])
     ref, rlse, _ = full_reference(few)
     rows_close(out[:, some], lse[:, some], ref, rlse, range(L), range(len(some)), "long runs")
+
+
+def test_shared_and_weighted_in_one_graph_on_a_side_stream():
+    """Both passes behind one another in one captured graph on a stream of its own, replayed with other lengths that share
+    nothing any more."""
+    seq = [900 + 40 * i for i in range(5)]
+    prob = make_problem(61, 2, 5, 8, 2, 128, seq)
+    share_prefixes(prob, [0, 5], [899])
+    ctx = gh.make_ctx(prob, [64] * 2, [4] * 2, [1] * 2)
+    dev = gh.upload(prob)
+    i32 = dict(dtype=torch.int32, device="cuda")
+    gs, gp, f = torch.tensor([0, 5], **i32), torch.tensor([899], **i32), torch.ones(5, **ONES)
+    out, lse = gh.new_out(prob, fill=-3.0)
+    out2, lse2 = gh.new_out(prob, fill=-3.0)
+    w = torch.zeros((2, 5, 2, prob["table"].shape[1] * 16), device="cuda")
+    side = torch.cuda.Stream()
+    s1, s2 = ctx.full_decode_shared_scratch(), ctx.full_decode_weighted_scratch()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=side):
+        ctx.full_decode_shared(0, 2, 5, dev["q"], dev["k"], dev["v"], dev["table"], dev["seq_lens"], f, gs, gp, out, lse, scratch=s1)
+        ctx.full_decode_weighted(0, 2, 5, dev["q"], dev["k"], dev["v"], dev["table"], dev["seq_lens"], f, w, out2, lse2, scratch=s2)
+    with torch.cuda.stream(side):
+        g.replay()
+    side.synchronize()
+    ref, rlse, _ = full_reference(prob)
+    rows_close(out, lse, ref, rlse, [0, 1], range(5), "shared")
+    rows_close(out2, lse2, ref, rlse, [0, 1], range(5), "weighted")
+    dev["seq_lens"].copy_(torch.tensor([1, 17, 900, 64, 1060]))
+    gp.copy_(torch.tensor([0]))
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        g.replay()
+    side.synchronize()
+    ref, rlse, _ = full_reference(dict(prob, seq_lens=np.array([1, 17, 900, 64, 1060], np.int32)))
+    rows_close(out, lse, ref, rlse, [0, 1], range(5), "shared, replayed")
+    rows_close(out2, lse2, ref, rlse, [0, 1], range(5), "weighted, replayed")
+    assert ctx.read_device_status() == 0
