@@ -5,7 +5,8 @@
 // x are the logits (log2 units) that the attention kernel left, (m, 1 / l) the finished softmax of each row.
 // The weights of a row are only known once its last page has been seen, so they cannot be added up inside the
 // pass; writing the logits (4 bytes a head and position) and reading them back costs 8 G of the 4 D bytes a
-// position that reading K a second time would half repeat.  Memory bound: 4 G + 8 bytes a position.
+// position that reading K a second time would half repeat.  Memory bound: 4 G + 8 bytes a position (32 layers of 8 heads,
+// 32,768 positions, G = 4: 201 MB, 30 us behind the pass's 673, 6.7 TB/s: the last logits come from L2).
 //
 // A position is added by one thread, heads in index order and layers that share a cache slice in layer order:
 // no atomics, the same bits every time.

@@ -12,7 +12,7 @@
 // Only whole pages are shared (a page that the prefix ends in is read through each request's own table row), and
 // every request keeps at least one position of its own, so the tail kernel leaves a row of every flagged request.
 //
-// Work: rows are cut into blocks of 256 (two 128-row MMA tiles), prefixes into tiles of kTokens positions; all
+// Work: rows are cut into blocks of one or two 128-row MMA tiles, prefixes into tiles of kTokens positions; all
 // (layer, kv head, group, row block, tile) lie on one axis that is cut into equal spans, one per CTA (one CTA per SM).
 // A unit that a span boundary cuts leaves several partials; nobody waits for another CTA.
 //
@@ -23,14 +23,24 @@
 //
 // Two forms of the kernel, chosen by the most rows that a kv head can have in the call (batch x group):
 //   narrow (<= 128 rows): bound by the stream of K and V.  One copy of Q, and the rest of shared memory as a ring.
-//   wide: bound by the products and the exponentials.  2 x 128 rows.
+//     32 layers, 16 requests of 4 heads, 8,192 positions, D = 128, bf16: 1.07 GB in 185 us, 5.8 TB/s.  D = 64 in fp32
+//     (three groups, 184 MB): 45 us without the waits of the launch, of which 5 until the first product, 4 where a span
+//     goes from one unit to the next, and the rest at 5.3 TB/s.
+//   wide: bound by the products and the exponentials.  2 x 128 rows.  8 layers, 64 requests of 8 heads, 32,768 positions,
+//     D = 128, bf16: 550 GFLOP in 535 us, 1.03 PFLOP/s in a short run; in a long one the power limit takes the
+//     clock down.  A tile (64 positions, 256 rows) takes 2,000 - 2,200 cycles.  Products need 1,280 of them: Q K^T reads
+//     both operands from shared memory, 48 cycles instead of 32 for 64 columns.  Exponentials need 1,024, 16 a cycle.
+//     Both streams do the same at the same time, so a warp's other 600 cycles (S to registers, maximum, barriers) do not hide
+//     behind the other's exponentials.
 // S has two buffers a stream (where TMEM holds them): while the softmax of a tile runs, the product for the stream's
 // next one is made, so that neither waits for the other.  With one, two row tiles fell into step -- both computed
 // exponentials, then both waited for products: 6,000 cycles for 128 positions -- and the narrow form spent
 // 2,400 cycles on the chain from one tile of a stream to its next.
 //
 // P in bf16 is kTerms parts of 8 bits each.  fp32 results take three (24 bits: nothing is lost against fp32
-// arithmetic), bf16 results two in the narrow form, where the second product hides behind the stream.
+// arithmetic), bf16 results two in the narrow form, where the second product hides behind the stream, and one in the
+// wide form, where it would be 256 more cycles of 1,280: P is then off by 2^-9 of each weight, as independent roundings
+// (the result's error against 64 bits is 0.0019 instead of 0.0017, most of it the result's own rounding).
 #include <cuda.h>
 
 #include <algorithm>
@@ -54,7 +64,6 @@ struct ShCfg {
     static constexpr int kTileBytes = kTokens * D * 2;      // K or V of one tile
     static constexpr int kSlotBytes = 2 * kTileBytes;       // V of a tile, and behind it the K that is needed next
     static constexpr int kSlots = (kWide ? 131072 : 196608) / kSlotBytes;
-    static constexpr int kRingSlots = kSlots / 2;           // slots of one stream's ring
     static_assert(kSlots % 2 == 0, "a stream and a producer keep to the slots of one parity");
     static constexpr int kQBytes = kShRows * D * 2;
     static constexpr int kQTiles = kWide ? 2 : 1;
@@ -282,7 +291,6 @@ __device__ __forceinline__ void shared_plan(const SharedParams& p, ShPlan& pl)
             d.total = max(pl.total, 1);
             d.nseg = pl.nseg;
         }
-        for (int l = tid; l < p.num_gated; l += blockDim.x) d.gated_index[p.layer[l]] = l;
         if (tid < B) {
             SharedRow r;
             r.unit = r.tiles = r.row = 0;
@@ -333,7 +341,7 @@ __device__ __forceinline__ ShItem shared_item(const SharedParams& p, const ShPla
 // seen the one before (or is joined with who has): a wait by parity cannot be answered by an older phase.
 template <int kSlots>
 __device__ __forceinline__ uint32_t ring_after(uint32_t parity, bool dual, int pos0, int pos1)
-    {
+{
 #pragma unroll
     for (int i = 0; i < kSlots; ++i) {
         const int n = dual ? (pos0 + kSlots - 1 - i) / kSlots
@@ -395,173 +403,174 @@ shared_prefix_kernel(const __grid_constant__ SharedParams p, const __grid_consta
     // (wide form: 384 x 168 registers were launched with; the softmax warps take what the others do not need:
     // 256 x 216 + 128 x 72)
     if (warp >= 8) {
-    if constexpr (kWide) asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
-    if (warp == 8 || warp == 11) {
-        // ============================ producer warps ============================
-        // Warp 8 fills the even slots, warp 11 the odd ones: a warp spends about 110 cycles on a box and 350 more on a
-        // slot, and DRAM delivers the 12 boxes of a slot (64 positions, D = 128) in 1,400.
-        const int half = warp == 8 ? 0 : 1;
-        const uint64_t once = 0x12F0000000000000ull;    // L2 evict-first: read by one row block
-        const uint64_t again = 0x1000000000000000ull;   // L2 evict-normal: the next row block reads it too
-        uint32_t parity = 0;
-        bool ok = true;
-        for (int x = x0; x < x1 && ok;) {
-            const ShItem it = shared_item<TP, C::kRowBlock>(p, pl, x, x1);
-            x += it.n;
-            const bool dual = kWide && it.nrows > kShRows;
-            const int lead_req = pl.g.list[pl.g.gs[it.group]];
-            const int32_t* table = p.block_table + (size_t)lead_req * p.max_blocks_per_seq;
-            const int first = it.tile0 * TP, last = min(it.pages, (it.tile0 + it.n) * TP);
-            const int kv0 = p.kv_index[it.gl] * p.blocks_per_layer;
-            const uint64_t policy = pl.g.members[it.group] * p.group > C::kRowBlock ? again : once;
-            // block ids of 32 pages from page `base` on and of the 32 behind them, one per lane; K runs ahead of V
-            struct Ids { int base, now, next; } ids_k, ids_v;
-            auto fetch = [&](int pg) { return pg + lane < last ? __ldg(table + pg + lane) : 0; };
-            ids_k.base = ids_v.base = first;
-            ids_k.now = ids_v.now = fetch(first);
-            ids_k.next = ids_v.next = fetch(first + 32);
-            auto block_of = [&](Ids& id, int pg, int pgi) {
-                if (pg - id.base >= 32) {
-                    id.base += 32;
-                    id.now = id.next;
-                    id.next = fetch(id.base + 32);
-                }
-                return kv0 + __shfl_sync(0xffffffffu, id.now, (pg - id.base + pgi) & 31);
-            };
-            // one slot: V of tile tv and K of tile tk (-1: none).  Lanes 0 .. TP-1 take a page of V each (one box: the page
-            // of the head, slab after slab), lanes 8 and up a page and slab of K (a slab's rows of all pages lie one
-            // behind the other).
-            auto load = [&](int tv, int tk, int slot, int round) {
-                const int e = lane - 8, ki = e % TP, slab = e / TP;
-                const int bv = tv >= 0 ? block_of(ids_v, first + tv * TP, lane) : 0;
-                const int bk = tk >= 0 ? block_of(ids_k, first + tk * TP, ki) : 0;
-                const bool mv = tv >= 0 && lane < TP && first + tv * TP + lane < last;
-                const bool mk = tk >= 0 && e >= 0 && e < kSlabs * TP && first + tk * TP + ki < last;
-                const uint32_t bytes = __popc(__ballot_sync(0xffffffffu, mv)) * (kPage * D * 2) + __popc(__ballot_sync(0xffffffffu, mk)) * (kPage * 128);
-                if (!warp_wait(&ctl.empty[slot], ((parity >> slot) ^ (uint32_t)round ^ 1u) & 1u, abort_flag, p.status)) return false;
-                const uint32_t bar = smem_u32(&ctl.full[slot]), dst = smem_u32(ring + slot * C::kSlotBytes);
-                if (lane == 0) mbar_expect_tx(bar, bytes);
-                __syncwarp();
-                if (mv || mk)
-                    tma_box(mv ? dst + lane * (kPage * D * 2) : dst + C::kTileBytes + slab * (TN * 128) + ki * 2048, mv ? &vmap : &kmap, bar,
-                            mv ? 0 : slab, it.kvh, mv ? bv : bk, policy);
-                return true;
-            };
-            // the positions of the slots that are this warp's: of the item (dual: every other one), or of its stream's tiles
-            const int step = dual ? 1 : 2, t0 = dual ? 0 : half;
-            const int nt = t0 < it.n ? (it.n - t0 + step - 1) / step : 0, lead = min(C::kBufs, nt);
-            int slot = half, round = 0;
-            for (int i = dual ? half : 0; i < lead + nt && ok; i += dual ? 2 : 1) {
-                const int j = i - lead;     // of the stream's tiles: V of the j-th, K of the (j + kBufs)-th
-                ok = load(j >= 0 ? t0 + j * step : -1, j < 0 ? t0 + i * step : j + C::kBufs < nt ? t0 + (j + C::kBufs) * step : -1, slot, round);
-                slot += 2;
-                if (slot >= C::kSlots) { slot = half; ++round; }
-            }
-            const int n1 = it.n / 2;        // (tiles of stream 1 where they take turns)
-            parity = dual ? ring_after<C::kSlots>(parity, true, lead + nt, 0)
-                          : ring_after<C::kSlots>(parity, false, it.n - n1 + min(C::kBufs, it.n - n1), n1 + min(C::kBufs, n1));
-        }
-        // Do not leave while copies may still be landing: every slot of this warp has been released since it was last
-        // filled (bounded; a slot that was never filled answers at once).
-        for (int slot = half; slot < C::kSlots && ok; slot += 2)
-            ok = warp_wait(&ctl.empty[slot], ((parity >> slot) & 1u) ^ 1u, abort_flag, p.status);
-    } else {
-        // ============================ MMA warps: one per stream, one thread issues ============================
-        // (The loop is run by the whole warp on warp-uniform values, and descriptors differ by constants: a thread
-        // that computes them anew before each product issues one in 100 cycles, slower than they run.  One warp for
-        // both streams spent 1470 cycles on a tile of 64 positions, most of them on its barriers.)
-        const int s = __reduce_max_sync(0xffffffffu, warp - 9);  // (a reduction's result is known to be uniform: descriptors stay in uniform registers)
-        constexpr uint32_t idesc_s = idesc_bf16(TN, false), idesc_o = idesc_bf16(D, true);
-        const bool leader = elect_one();
-        const uint32_t tm = __reduce_max_sync(0xffffffffu, tmem);
-        const uint32_t sp0 = tm + s * C::kBufs * C::kSpCols, to = tm + C::kO0 + s * D;  // S, then P; O
-        const uint32_t q_lo = smem_lo(smem_u32(qs), 16) + (kWide ? s : 0) * (C::kQBytes >> 4);
-        const uint32_t k_lo = smem_lo(smem_u32(ring) + C::kTileBytes, 16), v_lo = smem_lo(smem_u32(ring), 2048);
-        uint32_t parity = 0;
-        uint32_t nq = 0, np[2] = {0, 0};
-        bool ok = true;
-        for (int x = x0; x < x1 && ok;) {
-            const ShItem item = shared_item<TP, C::kRowBlock>(p, pl, x, x1);
-            x += item.n;
-            const int n = __reduce_max_sync(0xffffffffu, item.n);
-            const bool dual = kWide && __reduce_max_sync(0xffffffffu, item.nrows) > kShRows;
-            const int rest = __reduce_max_sync(0xffffffffu, item.pages - item.tile0 * TP);  // pages from the item's first on
-            const int step = dual ? 1 : 2, t0 = dual ? 0 : s;     // the stream's tiles: t0, t0 + step, ...
-            const int nt = t0 < n ? (n - t0 + step - 1) / step : 0;
-            constexpr int bufs = C::kBufs;
-            int slot = dual ? 0 : s, round = 0;
-            auto next_slot = [&]() {
-                slot += step;
-                if (slot >= C::kSlots) { slot = dual ? 0 : s; ++round; }
-            };
-            auto acquire = [&]() {
-                ok = warp_wait(&ctl.full[slot], ((parity >> slot) ^ (uint32_t)round) & 1u, abort_flag, p.status);
-                tc_fence_after();
-            };
-            auto release = [&]() {             // in the wide form a slot is free after two arrivals: one of each stream,
-                if (!leader) return;           // or both of the only one that reads it
-                tc_commit(smem_u32(&ctl.empty[slot]));
-                if (kWide && !dual) tc_commit(smem_u32(&ctl.empty[slot]));
-            };
-            auto qk = [&](int u) {             // whole tile (columns past the last page are not used)
-                const uint32_t b = k_lo + slot * (C::kSlotBytes >> 4), d = sp0 + u * C::kSpCols;
-                if (leader) {
-#pragma unroll
-                    for (int k = 0; k < D / 16; ++k)
-                        tc_mma_ss(d, q_lo + (k >> 2) * (kShRows * 128 >> 4) + (k & 3) * 2, b + (k >> 2) * (TN * 128 >> 4) + (k & 3) * 2,
-                                  kDescHi, idesc_s, k > 0);
-                    tc_commit(smem_u32(&ctl.s_full[s][u]));
-                }
-            };
-            if (nt > 0) {
-                ok = warp_wait(&ctl.q_full[s], nq++ & 1, abort_flag, p.status);
-                if (!ok) break;
-                tc_fence_after();
-            }
-            for (int i = 0; i < min(bufs, nt); ++i) {
-                acquire();
-                if (!ok) break;
-                qk(i);
-                release();
-                next_slot();
-            }
-            for (int i = 0; i < nt && ok; ++i) {
-                const int u = bufs == 2 ? i & 1 : 0;
-                acquire();
-                if (!ok) break;
-                const uint32_t ph = u ? np[1]++ : np[0]++;
-                ok = warp_wait(&ctl.p_full[s][u], ph & 1, abort_flag, p.status);
-                if (!ok) break;
-                tc_fence_after();
-                const int pages = min(TP, rest - (t0 + i * step) * TP);
-                const uint32_t b = v_lo + slot * (C::kSlotBytes >> 4), a = sp0 + u * C::kSpCols;
-                auto product = [&](int k) {    // a page is one K step of 16 positions
-#pragma unroll
-                    for (int c = 0; c < kTerms; ++c)
-                        tc_mma_ts(to, a + c * (TN / 2) + k * 8, b + k * (kPage * D * 2 >> 4), kDescHi, idesc_o, i > 0 || k + c > 0);
-                };
-                if (leader) {
-                    if (pages == TP) {
-#pragma unroll
-                        for (int k = 0; k < TP; ++k) product(k);
-                    } else {
-                        for (int k = 0; k < pages; ++k) product(k);
+        if constexpr (kWide) asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+        if (warp == 8 || warp == 11) {
+            // ============================ producer warps ============================
+            // Warp 8 fills the even slots, warp 11 the odd ones: a warp spends about 110 cycles on a box and 350 more on a
+            // slot, and DRAM delivers the 12 boxes of a slot (64 positions, D = 128) in 1,400.
+            const int half = warp == 8 ? 0 : 1;
+            const uint64_t once = 0x12F0000000000000ull;    // L2 evict-first: read by one row block
+            const uint64_t again = 0x1000000000000000ull;   // L2 evict-normal: the next row block reads it too
+            uint32_t parity = 0;
+            bool ok = true;
+            for (int x = x0; x < x1 && ok;) {
+                const ShItem it = shared_item<TP, C::kRowBlock>(p, pl, x, x1);
+                x += it.n;
+                const bool dual = kWide && it.nrows > kShRows;
+                const int lead_req = pl.g.list[pl.g.gs[it.group]];
+                const int32_t* table = p.block_table + (size_t)lead_req * p.max_blocks_per_seq;
+                const int first = it.tile0 * TP, last = min(it.pages, (it.tile0 + it.n) * TP);
+                const int kv0 = p.kv_index[it.gl] * p.blocks_per_layer;
+                const uint64_t policy = pl.g.members[it.group] * p.group > C::kRowBlock ? again : once;
+                // block ids of 32 pages from page `base` on and of the 32 behind them, one per lane; K runs ahead of V
+                struct Ids { int base, now, next; } ids_k, ids_v;
+                auto fetch = [&](int pg) { return pg + lane < last ? __ldg(table + pg + lane) : 0; };
+                ids_k.base = ids_v.base = first;
+                ids_k.now = ids_v.now = fetch(first);
+                ids_k.next = ids_v.next = fetch(first + 32);
+                auto block_of = [&](Ids& id, int pg, int pgi) {
+                    if (pg - id.base >= 32) {
+                        id.base += 32;
+                        id.now = id.next;
+                        id.next = fetch(id.base + 32);
                     }
+                    return kv0 + __shfl_sync(0xffffffffu, id.now, (pg - id.base + pgi) & 31);
+                };
+                // one slot: V of tile tv and K of tile tk (-1: none).  Lanes 0 .. TP-1 take a page of V each (one box: the page
+                // of the head, slab after slab), lanes 8 and up a page and slab of K (a slab's rows of all pages lie one
+                // behind the other).
+                auto load = [&](int tv, int tk, int slot, int round) {
+                    const int e = lane - 8, ki = e % TP, slab = e / TP;
+                    const int bv = tv >= 0 ? block_of(ids_v, first + tv * TP, lane) : 0;
+                    const int bk = tk >= 0 ? block_of(ids_k, first + tk * TP, ki) : 0;
+                    const bool mv = tv >= 0 && lane < TP && first + tv * TP + lane < last;
+                    const bool mk = tk >= 0 && e >= 0 && e < kSlabs * TP && first + tk * TP + ki < last;
+                    const uint32_t bytes = __popc(__ballot_sync(0xffffffffu, mv)) * (kPage * D * 2) + __popc(__ballot_sync(0xffffffffu, mk)) * (kPage * 128);
+                    if (!warp_wait(&ctl.empty[slot], ((parity >> slot) ^ (uint32_t)round ^ 1u) & 1u, abort_flag, p.status)) return false;
+                    const uint32_t bar = smem_u32(&ctl.full[slot]), dst = smem_u32(ring + slot * C::kSlotBytes);
+                    if (lane == 0) mbar_expect_tx(bar, bytes);
+                    __syncwarp();
+                    if (mv || mk)
+                        tma_box(mv ? dst + lane * (kPage * D * 2) : dst + C::kTileBytes + slab * (TN * 128) + ki * 2048, mv ? &vmap : &kmap, bar,
+                                mv ? 0 : slab, it.kvh, mv ? bv : bk, policy);
+                    return true;
+                };
+                // the positions of the slots that are this warp's: of the item (dual: every other one), or of its stream's tiles
+                const int step = dual ? 1 : 2, t0 = dual ? 0 : half;
+                const int nt = t0 < it.n ? (it.n - t0 + step - 1) / step : 0, lead = min(C::kBufs, nt);
+                int slot = half, round = 0;
+                for (int i = dual ? half : 0; i < lead + nt && ok; i += dual ? 2 : 1) {
+                    const int j = i - lead;     // of the stream's tiles: V of the j-th, K of the (j + kBufs)-th
+                    ok = load(j >= 0 ? t0 + j * step : -1, j < 0 ? t0 + i * step : j + C::kBufs < nt ? t0 + (j + C::kBufs) * step : -1, slot, round);
+                    slot += 2;
+                    if (slot >= C::kSlots) { slot = half; ++round; }
                 }
-                if (i + bufs < nt) {
-                    qk(u);                     // (S takes P's place: products of one thread run in order)
-                } else if (leader) {
-                    tc_commit(smem_u32(&ctl.pv_done[s][u]));
-                }
-                release();
-                next_slot();
+                const int n1 = it.n / 2;        // (tiles of stream 1 where they take turns)
+                parity = dual ? ring_after<C::kSlots>(parity, true, lead + nt, 0)
+                              : ring_after<C::kSlots>(parity, false, it.n - n1 + min(C::kBufs, it.n - n1), n1 + min(C::kBufs, n1));
             }
-            const int n1 = n / 2;
-            parity = dual ? ring_after<C::kSlots>(parity, true, nt + min(bufs, nt), 0)
-                          : ring_after<C::kSlots>(parity, false, n - n1 + min(bufs, n - n1), n1 + min(bufs, n1));
+            // Do not leave while copies may still be landing: every slot of this warp has been released since it was last
+            // filled (bounded; a slot that was never filled answers at once).
+            for (int slot = half; slot < C::kSlots && ok; slot += 2)
+                ok = warp_wait(&ctl.empty[slot], ((parity >> slot) & 1u) ^ 1u, abort_flag, p.status);
+        } else {
+            // ============================ MMA warps: one per stream, one thread issues ============================
+            // (The loop is run by the whole warp on warp-uniform values, and descriptors differ by constants: a thread
+            // that computes them anew before each product issues one in 100 cycles, slower than they run.  One warp for
+            // both streams spent 1470 cycles on a tile of 64 positions, most of them on its barriers.)
+            // (the result of a reduction is known to be uniform, that of a shuffle is not: descriptors stay in uniform registers)
+            const int s = __reduce_max_sync(0xffffffffu, warp - 9);
+            constexpr uint32_t idesc_s = idesc_bf16(TN, false), idesc_o = idesc_bf16(D, true);
+            const bool leader = elect_one();
+            const uint32_t tm = __reduce_max_sync(0xffffffffu, tmem);
+            const uint32_t sp0 = tm + s * C::kBufs * C::kSpCols, to = tm + C::kO0 + s * D;  // S, then P; O
+            const uint32_t q_lo = smem_lo(smem_u32(qs), 16) + (kWide ? s : 0) * (C::kQBytes >> 4);
+            const uint32_t k_lo = smem_lo(smem_u32(ring) + C::kTileBytes, 16), v_lo = smem_lo(smem_u32(ring), 2048);
+            uint32_t parity = 0;
+            uint32_t nq = 0, np[2] = {0, 0};
+            bool ok = true;
+            for (int x = x0; x < x1 && ok;) {
+                const ShItem item = shared_item<TP, C::kRowBlock>(p, pl, x, x1);
+                x += item.n;
+                const int n = __reduce_max_sync(0xffffffffu, item.n);
+                const bool dual = kWide && __reduce_max_sync(0xffffffffu, item.nrows) > kShRows;
+                const int rest = __reduce_max_sync(0xffffffffu, item.pages - item.tile0 * TP);  // pages from the item's first on
+                const int step = dual ? 1 : 2, t0 = dual ? 0 : s;     // the stream's tiles: t0, t0 + step, ...
+                const int nt = t0 < n ? (n - t0 + step - 1) / step : 0;
+                constexpr int bufs = C::kBufs;
+                int slot = dual ? 0 : s, round = 0;
+                auto next_slot = [&]() {
+                    slot += step;
+                    if (slot >= C::kSlots) { slot = dual ? 0 : s; ++round; }
+                };
+                auto acquire = [&]() {
+                    ok = warp_wait(&ctl.full[slot], ((parity >> slot) ^ (uint32_t)round) & 1u, abort_flag, p.status);
+                    tc_fence_after();
+                };
+                auto release = [&]() {             // in the wide form a slot is free after two arrivals: one of each stream,
+                    if (!leader) return;           // or both of the only one that reads it
+                    tc_commit(smem_u32(&ctl.empty[slot]));
+                    if (kWide && !dual) tc_commit(smem_u32(&ctl.empty[slot]));
+                };
+                auto qk = [&](int u) {             // whole tile (columns past the last page are not used)
+                    const uint32_t b = k_lo + slot * (C::kSlotBytes >> 4), d = sp0 + u * C::kSpCols;
+                    if (leader) {
+#pragma unroll
+                        for (int k = 0; k < D / 16; ++k)
+                            tc_mma_ss(d, q_lo + (k >> 2) * (kShRows * 128 >> 4) + (k & 3) * 2, b + (k >> 2) * (TN * 128 >> 4) + (k & 3) * 2,
+                                      kDescHi, idesc_s, k > 0);
+                        tc_commit(smem_u32(&ctl.s_full[s][u]));
+                    }
+                };
+                if (nt > 0) {
+                    ok = warp_wait(&ctl.q_full[s], nq++ & 1, abort_flag, p.status);
+                    if (!ok) break;
+                    tc_fence_after();
+                }
+                for (int i = 0; i < min(bufs, nt); ++i) {
+                    acquire();
+                    if (!ok) break;
+                    qk(i);
+                    release();
+                    next_slot();
+                }
+                for (int i = 0; i < nt && ok; ++i) {
+                    const int u = bufs == 2 ? i & 1 : 0;
+                    acquire();
+                    if (!ok) break;
+                    const uint32_t ph = u ? np[1]++ : np[0]++;
+                    ok = warp_wait(&ctl.p_full[s][u], ph & 1, abort_flag, p.status);
+                    if (!ok) break;
+                    tc_fence_after();
+                    const int pages = min(TP, rest - (t0 + i * step) * TP);
+                    const uint32_t b = v_lo + slot * (C::kSlotBytes >> 4), a = sp0 + u * C::kSpCols;
+                    auto product = [&](int k) {    // a page is one K step of 16 positions
+#pragma unroll
+                        for (int c = 0; c < kTerms; ++c)
+                            tc_mma_ts(to, a + c * (TN / 2) + k * 8, b + k * (kPage * D * 2 >> 4), kDescHi, idesc_o, i > 0 || k + c > 0);
+                    };
+                    if (leader) {
+                        if (pages == TP) {
+#pragma unroll
+                            for (int k = 0; k < TP; ++k) product(k);
+                        } else {
+                            for (int k = 0; k < pages; ++k) product(k);
+                        }
+                    }
+                    if (i + bufs < nt) {
+                        qk(u);                     // (S takes P's place: products of one thread run in order)
+                    } else if (leader) {
+                        tc_commit(smem_u32(&ctl.pv_done[s][u]));
+                    }
+                    release();
+                    next_slot();
+                }
+                const int n1 = n / 2;
+                parity = dual ? ring_after<C::kSlots>(parity, true, nt + min(bufs, nt), 0)
+                              : ring_after<C::kSlots>(parity, false, n - n1 + min(bufs, n - n1), n1 + min(bufs, n1));
+            }
+            __syncwarp();
         }
-        __syncwarp();
-    }
     } else {
         if constexpr (kWide) asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
         // ============================ softmax warpgroups: one thread per row ============================

@@ -20,7 +20,6 @@ struct __align__(16) SharedRow {   // one request
 // q_heads + head, chunk c > 0 at ext_row0 + (first span + c) * 256 + copy * (128 / copies) + row + head within the group.
 struct SharedDesc {
     int32_t t1, total, nseg, pad;    // tiles of one (layer, kv head), of all, spans they are cut into
-    int32_t gated_index[kMaxLayers]; // layer -> its place among the call's gated layers
     SharedRow rows[kMaxBatch];
 };
 
