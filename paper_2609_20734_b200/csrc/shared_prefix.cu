@@ -338,7 +338,8 @@ __device__ __forceinline__ ShItem shared_item(const SharedParams& p, const ShPla
 // tiles in slot 2 (i mod kSlots / 2) + s.  A stream's first positions hold the K tiles that run ahead of V alone, the
 // rest V of a tile with the K that comes next.  Every item begins at its first slots; `parity` has a bit per slot for
 // how often it has been filled.  So each slot is filled by one producer warp, and whoever waits for a filling has
-// seen the one before (or is joined with who has): a wait by parity cannot be answered by an older phase.
+// seen the one before, or has met who has (in the wide form streams meet after every item that is not dual, a lone tile
+// too): a wait by parity cannot be answered by an older phase.
 template <int kSlots>
 __device__ __forceinline__ uint32_t ring_after(uint32_t parity, bool dual, int pos0, int pos1)
 {
@@ -679,7 +680,15 @@ shared_prefix_kernel(const __grid_constant__ SharedParams p, const __grid_consta
             const ShItem it = shared_item<TP, C::kRowBlock>(p, pl, x, x1);
             x += it.n;
             const bool dual = kWide && it.nrows > kShRows;
-            if (!dual && s == 1 && it.n == 1) continue;  // a lone tile: stream 0's
+            if (!dual && s == 1 && it.n == 1) {  // a lone tile: stream 0's
+                if constexpr (kWide) {
+                    // A dual item that follows uses the slot that this tile is in: a stream that went ahead would take an
+                    // older filling of that slot for its own.
+                    if (lane == 0) mbar_arrive(smem_u32(&ctl.ml_full));
+                    if (!warp_wait(&ctl.o1_read, nj++ & 1, abort_flag, p.status)) ok = false;
+                }
+                continue;
+            }
             const int copies = kWide ? 1 : row_copies(it.nrows), per_copy = kShRows / copies;
             const int copy = kWide ? 0 : tr / per_copy;
             const int row = dual ? s * kShRows + tr : kWide ? tr : tr % per_copy;
@@ -738,8 +747,9 @@ shared_prefix_kernel(const __grid_constant__ SharedParams p, const __grid_consta
             if (!ok) break;
             tc_fence_after();
             // ---- the item's partial: chunk 0 of a unit in the row's own place, later chunks in the span's ----
-            const bool joined = !dual && it.n > 1;
+            const bool joined = !dual && it.n > 1, meet = !dual && (kWide || it.n > 1);
             float a0 = 1.f, a1 = 0.f;
+            if (kWide && meet && !joined && !warp_wait(&ctl.ml_full, nj & 1, abort_flag, p.status)) { ok = false; break; }
             if (joined) {
                 if (s == 1) {
                     const uint32_t v[2] = {__float_as_uint(m), __float_as_uint(l)};  // left in its own, now unused, S
@@ -784,7 +794,7 @@ shared_prefix_kernel(const __grid_constant__ SharedParams p, const __grid_consta
                 if (valid) __stcg(p.part_ml + dst, make_float2(m, l));
             }
             tc_fence_before();
-            if (joined) {  // stream 1's next item may overwrite its O and (m, l) once stream 0 has read them
+            if (meet) {    // stream 1's next item may overwrite its O and (m, l) once stream 0 has read them
                 __syncwarp();
                 if (s == 0) {
                     if (lane == 0) mbar_arrive(smem_u32(&ctl.o1_read));

@@ -247,3 +247,27 @@ def test_shared_and_weighted_in_one_graph_on_a_side_stream():
     rows_close(out, lse, ref, rlse, [0, 1], range(5), "shared, replayed")
     rows_close(out2, lse2, ref, rlse, [0, 1], range(5), "weighted, replayed")
     assert ctx.read_device_status() == 0
+
+
+def test_shared_one_tile_of_two_blocks_of_rows_many_times():
+    """Prefixes of one tile whose rows are a block for both row tiles and a rest for one: a CTA changes between the two kinds
+    of item at every tile, and no stream may be ahead of the other across the change.  Against the plain gated pass, and
+    the same bits every time."""
+    L, B, Hq, Hkv, D = 96, 99, 64, 8, 64
+    seq = [64 + 1 + i % 9 for i in range(B)]
+    prob = make_problem(62, 1, B, Hq, Hkv, D, seq)
+    share_prefixes(prob, [0, 33, 66, 99], [64] * 3)
+    prob = dict(prob, L=L, q=synth.gauss_bf16_tensor(63, synth.STREAM_Q, (L, B, Hq, D)))
+    ctx = gh.make_ctx(prob, [16] * L, [0] * L, [1] * L, kv_index=[0] * L)
+    dev = gh.upload(prob)
+    f = torch.ones(B, **ONES)
+    want, wlse = gh.new_out(prob)
+    ctx.full_decode_gated(0, L, B, dev["q"], dev["k"], dev["v"], dev["table"], dev["seq_lens"], f, want, wlse)
+    first = None
+    for _ in range(40):
+        _, out, lse = run_shared(prob, [0, 33, 66, 99], [64] * 3, [1] * B, ctx=ctx, dev=dev)
+        if first is None:
+            first = (out, lse)
+            assert (out - want).abs().max() <= gh.ATOL_OUT and (lse - wlse).abs().max() <= gh.ATOL_LSE
+        assert torch.equal(out, first[0]) and torch.equal(lse, first[1])
+    assert ctx.read_device_status() == 0
