@@ -407,7 +407,7 @@ oda_status_t oda_full_decode_weighted(oda_ctx_t* ctx, int32_t layer_begin, int32
  *     256-byte aligned, oda_evict_scratch_bytes(ctx) suffices for every budget); with it scratch may be NULL.
  *   weights: as in oda_full_decode_weighted, 16-byte aligned (a kept -0 may become 0, a NaN another NaN).  All slices
  *     of the cache are treated, those of fixed-window layers too: choose `recent` at least as large as the largest
- *     window, and what a Local pass reads stays what it was.
+ *     window and `sinks` at least as the most sinks, and what a Local pass reads stays what it was.
  * The rows move inside the request's own pages: no other request may use a page of a request that is shortened
  * (a shared prefix is copied before its first eviction).  Pages behind the budget are free afterwards; the block table
  * is not changed.  Requires 1 <= budget <= max_blocks_per_seq * 16 and 0 <= sinks + recent <= budget.  A request with
